@@ -285,6 +285,43 @@ DISCO_API int disco_logit_scale_fwd(const float* theta, float s_max, float* s, v
 DISCO_API int disco_logit_scale_bwd(const float* theta, float s_max, const float* gs, float* gtheta, int accumulate,
                                     void* hip_stream);
 
+/*
+ * Operators of the towers on either side of the loss (Alg. 1's first and last segment: encoders, backward on the features), and of the
+ * end of the backward pass.  As everywhere here: device pointers owned by the caller, work on hip_stream, nothing allocated, nothing
+ * kept after the call, kernels only (so a call may be captured), errors as status codes before anything is launched.
+ *
+ * Attention over packed sequences.  Rows starts[s] .. starts[s + 1] of q, k, v and o are sequence s (starts: sequences + 1 int32 on the
+ * device, not decreasing, from 0 or later to `tokens` or earlier; a sequence may be empty).  Query head h reads key/value head
+ * h / (heads / kv_heads).  Element (row, head, channel) of q is at row q_row + head q_head + channel, and so on; dq lies as q, dk as k, dv
+ * as v, dout as o.
+ *   o_i = sum_j P_ij v_j,  P_ij = exp(scale <q_i, k_j> - lse_i),  lse_i = log sum_j exp(scale <q_i, k_j>),  over the keys j of row i's sequence,
+ *   those up to i if `causal`.
+ * q, k, v, o and the gradients are bf16 (dtype DISCO_BF16); lse is heads x tokens fp32, kept for the backward pass.  Scores, softmax and sums are
+ * fp32, the softmax values and their gradients are rounded to bf16 before they are multiplied by v, dout, k and q.
+ * Rows before the first and behind the last sequence are neither read nor written.  A NaN or infinity stays within its sequence; inside it, one in a
+ * value row can reach earlier rows of a causal sequence too (up to 31 before it), as 0 times NaN.
+ * All 16 bytes aligned, strides multiples of 8; head_dim a multiple of 8 up to 128 (else DISCO_ERR_UNSUPPORTED).  tokens < 2^31,
+ * sequences <= 2^24, heads <= 2^16, (tokens / 32 + sequences) heads < 2^31, scale > 0, strides in 1 .. 2^31 (else DISCO_ERR_SHAPE).  Outputs overlap
+ * nothing else (q, k, v may be views of one buffer, and so may dq, dk, dv).  Equal calls give equal bits.
+ *
+ * disco_attention_bwd takes what the forward call read and wrote, and dout = d loss / d o.  workspace: disco_attention_workspace_bytes (0: invalid
+ * shape), 256-byte aligned, heads x tokens fp32.
+ */
+typedef struct {
+  int64_t tokens;
+  int32_t sequences, heads, kv_heads, head_dim;
+  int32_t causal;            /* 0 or 1 */
+  int32_t dtype;             /* DISCO_BF16 */
+  float scale;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;   /* in elements */
+} disco_attention_shape;
+DISCO_API size_t disco_attention_workspace_bytes(const disco_attention_shape* shape);
+DISCO_API int disco_attention_fwd(const disco_attention_shape* shape, const int32_t* starts, const void* q, const void* k, const void* v,
+                                  void* o, float* lse, void* hip_stream);
+DISCO_API int disco_attention_bwd(const disco_attention_shape* shape, const int32_t* starts, const void* q, const void* k, const void* v,
+                                  const void* o, const float* lse, const void* dout, void* dq, void* dk, void* dv, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream);
+
 /* Static, NUL-terminated description of a status code. */
 DISCO_API const char* disco_status_string(int status);
 

@@ -32,6 +32,13 @@ class DiscoPlan(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_uint64)]
 
 
+class DiscoAttention(ctypes.Structure):
+    """disco_attention_shape."""
+    _fields_ = [("tokens", ctypes.c_int64), ("sequences", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)] + [
+                    (m + "_" + way, ctypes.c_int64) for m in "qkvo" for way in ("row", "head")]
+
+
 class DiscoError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -78,6 +85,13 @@ def _load():
     lib.disco_logit_scale_fwd.restype = ci
     lib.disco_logit_scale_bwd.argtypes = [vp, f32, vp, vp, ci, vp]
     lib.disco_logit_scale_bwd.restype = ci
+    attention = ctypes.POINTER(DiscoAttention)
+    lib.disco_attention_workspace_bytes.argtypes = [attention]
+    lib.disco_attention_workspace_bytes.restype = sz
+    lib.disco_attention_fwd.argtypes = [attention] + [vp] * 7
+    lib.disco_attention_fwd.restype = ci
+    lib.disco_attention_bwd.argtypes = [attention] + [vp] * 11 + [sz, vp]
+    lib.disco_attention_bwd.restype = ci
     lib.disco_describe_plan.argtypes = [i64, i64, i32, ci, ci, ci, sz, ctypes.POINTER(DiscoPlan)]
     lib.disco_describe_plan.restype = ci
     lib.disco_mfma_probe.argtypes = [ci, ci, ci, vp, vp, vp]
@@ -212,4 +226,23 @@ def disco_logit_scale_bwd(theta, s_max, gs, gtheta, accumulate=0, stream=None, c
     st = _lib.disco_logit_scale_bwd(_ptr(theta), s_max, _ptr(gs), _ptr(gtheta), int(accumulate), _stream_ptr(stream))
     if check and st != DISCO_OK:
         raise DiscoError(st, "disco_logit_scale_bwd")
+    return st
+
+
+def disco_attention_workspace_bytes(shape: DiscoAttention) -> int:
+    return _lib.disco_attention_workspace_bytes(ctypes.byref(shape))
+
+
+def disco_attention_fwd(shape, starts, q, k, v, o, lse, stream=None, check=True) -> int:
+    st = _lib.disco_attention_fwd(ctypes.byref(shape), _ptr(starts), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _stream_ptr(stream))
+    if check and st != DISCO_OK:
+        raise DiscoError(st, "disco_attention_fwd")
+    return st
+
+
+def disco_attention_bwd(shape, starts, q, k, v, o, lse, dout, dq, dk, dv, workspace, workspace_bytes, stream=None, check=True) -> int:
+    st = _lib.disco_attention_bwd(ctypes.byref(shape), _ptr(starts), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(dout), _ptr(dq),
+                                  _ptr(dk), _ptr(dv), _ptr(workspace), workspace_bytes, _stream_ptr(stream))
+    if check and st != DISCO_OK:
+        raise DiscoError(st, "disco_attention_bwd")
     return st

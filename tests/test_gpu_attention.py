@@ -1,0 +1,177 @@
+"""disco_attention_fwd and disco_attention_bwd against the float64 oracle, every entry within the bound that the oracle derives for it."""
+import pytest
+import torch
+
+import paper_2304_08480_amd as dl
+from oracle import attention as oa
+
+pytestmark = pytest.mark.gpu
+
+
+class Attention:
+    """Buffers of one packed batch: a fused projection output, or separate tensors with room between rows and heads."""
+
+    def __init__(self, lengths, heads, kv_heads, dim, causal, seed=0, first=0, behind=0, fused=True, scale=None, gap=0, sharp=1.0):
+        g = torch.Generator().manual_seed(seed)
+        starts = [first]
+        for n in lengths:
+            starts.append(starts[-1] + n)
+        T = starts[-1] + behind
+        self.T, self.H, self.G, self.D, self.causal, self.starts_host = T, heads, kv_heads, dim, causal, starts
+        self.scale = dim ** -0.5 if scale is None else scale
+
+        def make(n, spread=1.0):
+            return (torch.randn(T, n, dim, generator=g) * spread).to(torch.bfloat16)
+
+        self.host = [make(heads, sharp), make(kv_heads), make(kv_heads), make(heads)]
+        self.starts = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        row = {"q": heads, "k": kv_heads, "v": kv_heads, "o": heads}
+        if fused:
+            buffer = torch.cat(self.host[:3], 1).cuda()
+            grads = torch.full_like(buffer, float("nan"))
+            cut = (heads, kv_heads, kv_heads)
+            self.q, self.k, self.v = buffer.split(cut, 1)
+            self.dq, self.dk, self.dv = grads.split(cut, 1)
+            self.do = self.host[3].cuda()
+            self.o = torch.full_like(self.do, float("nan"))
+        else:
+            def place(t, n):
+                wide = torch.full((T, n + 1, dim + gap), float("nan"), dtype=torch.bfloat16, device="cuda")
+                view = wide[:, :n, :dim]
+                if t is not None:
+                    view.copy_(t)
+                return view
+
+            self.q, self.k, self.v, self.do = (place(t, t.shape[1]) for t in self.host)
+            self.o, self.dq, self.dk, self.dv = (place(None, n) for n in (heads, heads, kv_heads, kv_heads))
+        self.lse = torch.full((heads, T), float("nan"), device="cuda")
+        strides = {m + "_" + way: getattr(self, m).stride(i) for m in row for i, way in enumerate(("row", "head"))}
+        self.shape = dl.DiscoAttention(tokens=T, sequences=len(lengths), heads=heads, kv_heads=kv_heads, head_dim=dim, causal=int(causal),
+                                       dtype=dl.DISCO_BF16, scale=self.scale, **strides)
+        self.need = dl.disco_attention_workspace_bytes(self.shape)
+        self.ws = torch.full((self.need,), 255, dtype=torch.uint8, device="cuda")
+
+    def forward(self, stream=None):
+        dl.disco_attention_fwd(self.shape, self.starts, self.q, self.k, self.v, self.o, self.lse, stream or torch.cuda.current_stream())
+
+    def backward(self, stream=None):
+        dl.disco_attention_bwd(self.shape, self.starts, self.q, self.k, self.v, self.o, self.lse, self.do, self.dq, self.dk, self.dv, self.ws,
+                               self.need, stream or torch.cuda.current_stream())
+
+    def outputs(self):
+        return {n: getattr(self, n).float().cpu() for n in ("o", "lse", "dq", "dk", "dv")}
+
+    def check(self):
+        want = oa.packed(*(t.double() for t in self.host[:3]), self.starts_host, self.scale, self.causal, self.host[3].double())
+        for name, got in self.outputs().items():
+            value, bound = want[name]
+            outside = torch.isinf(bound)
+            assert torch.isnan(got[outside]).all(), name + ": rows of no sequence were written"
+            off = (got.double() - value).abs()[~outside] / bound[~outside].clamp(min=1e-30)
+            assert not off.numel() or float(off.max()) <= 1.0, (name, float(off.max()))
+
+
+LENGTHS = [[1], [2, 1], [31], [32], [33], [64, 0, 65], [127, 128, 129], [5, 0, 0, 77, 1, 30], [300, 1, 200]]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("dim", [64, 128])
+def test_lengths(lengths, dim, causal):
+    print("case attention", lengths, dim, causal, flush=True)
+    a = Attention(lengths, 4, 2, dim, causal, seed=len(lengths))
+    a.forward()
+    a.backward()
+    a.check()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dim", [8, 16, 24, 32, 40, 56, 72, 80, 96, 104, 120])
+@pytest.mark.parametrize("lengths", [[3, 40, 9], [70, 140]], ids=str)
+def test_head_widths(lengths, dim, causal):
+    print("case attention width", lengths, dim, causal, flush=True)
+    a = Attention(lengths, 3, 3, dim, causal, seed=dim)
+    a.forward()
+    a.backward()
+    a.check()
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (5, 1), (6, 2), (8, 8), (12, 3)])
+def test_shared_heads_strides_and_rows_of_no_sequence(heads, kv_heads):
+    print("case attention heads", heads, kv_heads, flush=True)
+    for lengths in ([17, 33, 64], [200, 111]):
+        a = Attention(lengths, heads, kv_heads, 64, True, seed=heads, first=5, behind=9, fused=False, gap=8)
+        a.forward()
+        a.backward()
+        a.check()
+
+
+@pytest.mark.parametrize("scale,sharp", [(1e-3, 1.0), (0.125, 12.0), (2.0, 3.0)])
+def test_flat_and_saturated_softmax(scale, sharp):
+    a = Attention([90, 150], 2, 2, 64, True, scale=scale, sharp=sharp)
+    a.forward()
+    a.backward()
+    a.check()
+
+
+def test_thousands_of_short_sequences():
+    g = torch.Generator().manual_seed(3)
+    lengths = torch.randint(0, 9, (5000,), generator=g).tolist()
+    a = Attention(lengths, 2, 1, 32, True)
+    a.forward()
+    a.backward()
+    a.check()
+
+
+def test_equal_calls_give_equal_bits_and_neighbours_do_not_matter():
+    a = Attention([50, 0, 300, 77], 4, 2, 64, True)
+    a.forward()
+    a.backward()
+    one = a.outputs()
+    a.forward()
+    a.backward()
+    assert all(torch.equal(one[n], x) for n, x in a.outputs().items())
+    # what is not finite stays within its sequence
+    for t in (a.q, a.k, a.v, a.do):
+        t[50:60] = float("nan")
+        t[345:350] = float("inf")
+    a.forward()
+    a.backward()
+    for n, x in a.outputs().items():
+        y = one[n]
+        if n == "lse":
+            x, y = x.T, y.T
+        assert torch.equal(x[:50], y[:50]) and torch.equal(x[350:], y[350:]), n
+        assert torch.isnan(x[50:350]).any()
+
+
+def test_captured_and_on_another_stream():
+    a, b = (Attention([40, 90, 3], 4, 2, 64, True, seed=s) for s in (1, 2))
+    eager = []
+    for x in (a, b):
+        x.forward()
+        x.backward()
+        eager.append(x.outputs())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for x in (a, b):
+            x.forward()
+            x.backward()
+    for _ in range(3):
+        for x in (a, b):
+            for t in (x.o, x.lse, x.dq, x.dk, x.dv):
+                t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, want in zip((a, b), eager):
+            assert all(torch.equal(want[n], y) for n, y in x.outputs().items())
+    # two calls at once
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for x, s in zip((a, b), streams):
+        with torch.cuda.stream(s):
+            x.forward(s)
+            x.backward(s)
+    torch.cuda.synchronize()
+    for x, want in zip((a, b), eager):
+        assert all(torch.equal(want[n], y) for n, y in x.outputs().items())
