@@ -298,8 +298,8 @@ DISCO_API int disco_logit_scale_bwd(const float* theta, float s_max, const float
  *   those up to i if `causal`.
  * q, k, v, o and the gradients are bf16 (dtype DISCO_BF16); lse is heads x tokens fp32, kept for the backward pass.  Scores, softmax and sums are
  * fp32, the softmax values and their gradients are rounded to bf16 before they are multiplied by v, dout, k and q.
- * Rows before the first and behind the last sequence are neither read nor written.  A NaN or infinity stays within its sequence; inside it, one in a
- * value row can reach earlier rows of a causal sequence too (up to 31 before it), as 0 times NaN.
+ * Rows before the first and behind the last sequence are neither read nor written.  A NaN or infinity stays within its sequence; inside it, one can also
+ * reach rows up to 31 away that the mask hides from it, as 0 times NaN.
  * All 16 bytes aligned, strides multiples of 8; head_dim a multiple of 8 up to 128 (else DISCO_ERR_UNSUPPORTED).  tokens < 2^31,
  * sequences <= 2^24, heads <= 2^16, (tokens / 32 + sequences) heads < 2^31, scale > 0, strides in 1 .. 2^31 (else DISCO_ERR_SHAPE).  Outputs overlap
  * nothing else (q, k, v may be views of one buffer, and so may dq, dk, dv).  Equal calls give equal bits.
@@ -321,6 +321,56 @@ DISCO_API int disco_attention_fwd(const disco_attention_shape* shape, const int3
 DISCO_API int disco_attention_bwd(const disco_attention_shape* shape, const int32_t* starts, const void* q, const void* k, const void* v,
                                   const void* o, const float* lse, const void* dout, void* dq, void* dk, void* dv, void* workspace,
                                   size_t workspace_bytes, void* hip_stream);
+
+/*
+ * What stands between two blocks of a tower: the norm after a block, its gate and residual scale, the residual sum and the norm before the next
+ * block, for rows x d (row-major, contiguous; d <= 8192).
+ *   u = N_post(h), or h if post is DISCO_NORM_NONE;   y = x_scale x + h_scale gate u;   n = N_pre(y), of y as it is stored
+ *   N(z) = (z - mean) / sqrt(var + eps) w + b (DISCO_NORM_LAYER), z / sqrt(mean(z^2) + eps) w + b (DISCO_NORM_RMS); w NULL: 1, b NULL: 0
+ * x, y, dx, dy have x_dtype; h, n, dh, dn and a gate for each element h_dtype; norm parameters, a gate for each channel, their gradients and the
+ * statistics are fp32.  x NULL: y is the branch alone.  n is not written without a norm before the next block.
+ * stats: rows x 4 (mean and 1 / sqrt(var + eps) of h, then of y; 0 where there is none), kept for the backward pass.
+ *
+ * disco_block_norm_bwd: dy = d loss / d y from the stream (NULL: none, if there is a dn), dn = d loss / d n, h, y, gate, parameters and stats of the
+ * forward call (those that the formulas use: y and dn with a norm before the next block, h with a norm after the block or a gate).  Writes dx (NULL: not wanted), dh, and where not NULL dgate (as gate), dw_post, db_post, dw_pre, db_pre: sums over all rows, in a fixed
+ * order (equal calls give equal bits).  workspace: disco_block_norm_workspace_bytes (0: invalid shape), 256-byte aligned.
+ * Each row's loads come before its stores, so in either call an output may be one of its inputs of the same type (y = x, n = h, dx = dy, dh = dn).
+ * A NaN or infinity stays within its row, and in the sums over rows.
+ */
+typedef enum { DISCO_NORM_NONE = 0, DISCO_NORM_LAYER = 1, DISCO_NORM_RMS = 2 } disco_norm;
+typedef enum { DISCO_GATE_NONE = 0, DISCO_GATE_CHANNEL = 1 /* d fp32 */, DISCO_GATE_ELEMENT = 2 /* rows x d */ } disco_gate;
+typedef struct {
+  int64_t rows, d;
+  int32_t post, pre;         /* disco_norm */
+  int32_t gate;              /* disco_gate */
+  int32_t x_dtype, h_dtype;  /* disco_dtype */
+  float eps_post, eps_pre;   /* >= 0 */
+  float x_scale, h_scale;
+} disco_block_norm_shape;
+DISCO_API size_t disco_block_norm_workspace_bytes(const disco_block_norm_shape* shape);
+DISCO_API int disco_block_norm_fwd(const disco_block_norm_shape* shape, const void* x, const void* h, const void* gate, const float* w_post,
+                                   const float* b_post, const float* w_pre, const float* b_pre, void* y, void* n, float* stats, void* hip_stream);
+DISCO_API int disco_block_norm_bwd(const disco_block_norm_shape* shape, const void* dy, const void* dn, const void* h, const void* y,
+                                   const void* gate, const float* w_post, const float* b_post, const float* w_pre, const float* stats, void* dx,
+                                   void* dh, void* dgate, float* dw_post, float* db_post, float* dw_pre, float* db_pre, void* workspace,
+                                   size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The global norm of a step's gradients, and clipping by it.  A list of `count` tensors is four host arrays that are read during the call: device
+ * pointers, numbers of elements (>= 0, a pointer may be NULL where it is 0), types (disco_dtype; gradients of different types may be mixed).
+ *
+ * disco_grad_norm: *norm = sqrt(sum of all squares), or with accumulate sqrt(*norm^2 + that sum), for lists that are taken in parts.  Squares are summed
+ * in fp64 in a fixed order: no gradient that fp32 holds overflows or underflows, equal calls give equal bits.
+ * disco_grad_clip: dst = src * min(1, max_norm / (norm + 1e-6)), in fp32, rounded to the tensor's type; dst[i] may be src[i], else they overlap nothing.
+ * The norm is *given where given is not NULL (of more lists than this one, or of several GPUs), else that of src, taken by the same call.  *norm becomes
+ * the norm taken either way (before clipping; norm may be given).  A norm of NaN makes every dst NaN, one of infinity makes finite gradients 0.
+ * workspace: disco_grad_workspace_bytes(count) (0: count < 0 or > 2^20), 256-byte aligned.  max_norm > 0 (infinity: nothing is clipped).
+ */
+DISCO_API size_t disco_grad_workspace_bytes(int64_t count);
+DISCO_API int disco_grad_norm(const void* const* src, const int64_t* elements, const int32_t* dtypes, int64_t count, int accumulate, float* norm,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+DISCO_API int disco_grad_clip(const void* const* src, void* const* dst, const int64_t* elements, const int32_t* dtypes, int64_t count,
+                              float max_norm, const float* given, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Static, NUL-terminated description of a status code. */
 DISCO_API const char* disco_status_string(int status);

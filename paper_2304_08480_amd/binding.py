@@ -16,6 +16,8 @@ import torch  # noqa: F401  (import order matters)
 DISCO_OK = 0
 DISCO_ERR_NULL, DISCO_ERR_SHAPE, DISCO_ERR_UNSUPPORTED, DISCO_ERR_WORKSPACE, DISCO_ERR_HIP = 1, 2, 3, 4, 5
 DISCO_F32, DISCO_BF16 = 0, 1
+DISCO_NORM_NONE, DISCO_NORM_LAYER, DISCO_NORM_RMS = 0, 1, 2
+DISCO_GATE_NONE, DISCO_GATE_CHANNEL, DISCO_GATE_ELEMENT = 0, 1, 2
 DISCO_PATH_AUTO, DISCO_PATH_NAIVE, DISCO_PATH_MATERIALIZED, DISCO_PATH_FUSED, DISCO_PATH_SYMMETRIC = 0, 1, 2, 3, 4
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -37,6 +39,13 @@ class DiscoAttention(ctypes.Structure):
     _fields_ = [("tokens", ctypes.c_int64), ("sequences", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)] + [
                     (m + "_" + way, ctypes.c_int64) for m in "qkvo" for way in ("row", "head")]
+
+
+class DiscoBlockNorm(ctypes.Structure):
+    """disco_block_norm_shape."""
+    _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int64), ("post", ctypes.c_int32), ("pre", ctypes.c_int32), ("gate", ctypes.c_int32),
+                ("x_dtype", ctypes.c_int32), ("h_dtype", ctypes.c_int32), ("eps_post", ctypes.c_float), ("eps_pre", ctypes.c_float),
+                ("x_scale", ctypes.c_float), ("h_scale", ctypes.c_float)]
 
 
 class DiscoError(RuntimeError):
@@ -92,6 +101,19 @@ def _load():
     lib.disco_attention_fwd.restype = ci
     lib.disco_attention_bwd.argtypes = [attention] + [vp] * 11 + [sz, vp]
     lib.disco_attention_bwd.restype = ci
+    block_norm = ctypes.POINTER(DiscoBlockNorm)
+    lib.disco_block_norm_workspace_bytes.argtypes = [block_norm]
+    lib.disco_block_norm_workspace_bytes.restype = sz
+    lib.disco_block_norm_fwd.argtypes = [block_norm] + [vp] * 11
+    lib.disco_block_norm_fwd.restype = ci
+    lib.disco_block_norm_bwd.argtypes = [block_norm] + [vp] * 17 + [sz, vp]
+    lib.disco_block_norm_bwd.restype = ci
+    lib.disco_grad_workspace_bytes.argtypes = [i64]
+    lib.disco_grad_workspace_bytes.restype = sz
+    lib.disco_grad_norm.argtypes = [vp, vp, vp, i64, ci, vp, vp, sz, vp]
+    lib.disco_grad_norm.restype = ci
+    lib.disco_grad_clip.argtypes = [vp, vp, vp, vp, i64, f32, vp, vp, vp, sz, vp]
+    lib.disco_grad_clip.restype = ci
     lib.disco_describe_plan.argtypes = [i64, i64, i32, ci, ci, ci, sz, ctypes.POINTER(DiscoPlan)]
     lib.disco_describe_plan.restype = ci
     lib.disco_mfma_probe.argtypes = [ci, ci, ci, vp, vp, vp]
@@ -245,4 +267,71 @@ def disco_attention_bwd(shape, starts, q, k, v, o, lse, dout, dq, dk, dv, worksp
                                   _ptr(dk), _ptr(dv), _ptr(workspace), workspace_bytes, _stream_ptr(stream))
     if check and st != DISCO_OK:
         raise DiscoError(st, "disco_attention_bwd")
+    return st
+
+
+def disco_block_norm_workspace_bytes(shape: DiscoBlockNorm) -> int:
+    return _lib.disco_block_norm_workspace_bytes(ctypes.byref(shape))
+
+
+def disco_block_norm_fwd(shape, x, h, gate, w_post, b_post, w_pre, b_pre, y, n, stats, stream=None, check=True) -> int:
+    st = _lib.disco_block_norm_fwd(ctypes.byref(shape), _ptr(x), _ptr(h), _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre), _ptr(b_pre),
+                                   _ptr(y), _ptr(n), _ptr(stats), _stream_ptr(stream))
+    if check and st != DISCO_OK:
+        raise DiscoError(st, "disco_block_norm_fwd")
+    return st
+
+
+def disco_block_norm_bwd(shape, dy, dn, h, y, gate, w_post, b_post, w_pre, stats, dx, dh, dgate, dw_post, db_post, dw_pre, db_pre, workspace,
+                         workspace_bytes, stream=None, check=True) -> int:
+    st = _lib.disco_block_norm_bwd(ctypes.byref(shape), _ptr(dy), _ptr(dn), _ptr(h), _ptr(y), _ptr(gate), _ptr(w_post), _ptr(b_post),
+                                   _ptr(w_pre), _ptr(stats), _ptr(dx), _ptr(dh), _ptr(dgate), _ptr(dw_post), _ptr(db_post), _ptr(dw_pre),
+                                   _ptr(db_pre), _ptr(workspace), workspace_bytes, _stream_ptr(stream))
+    if check and st != DISCO_OK:
+        raise DiscoError(st, "disco_block_norm_bwd")
+    return st
+
+
+_DTYPES = {torch.float32: DISCO_F32, torch.bfloat16: DISCO_BF16}
+
+
+def _addresses(tensors):
+    return (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+
+
+def _listed(tensors):
+    """Host arrays of a list of dense torch tensors: addresses, numbers of elements, types (-1, which the library refuses, where it has none)."""
+    n = len(tensors)
+    for t in tensors:
+        if not t.is_contiguous():
+            raise ValueError("gradients have to be contiguous")
+    return (_addresses(tensors), (ctypes.c_int64 * n)(*[t.numel() for t in tensors]),
+            (ctypes.c_int32 * n)(*[_DTYPES.get(t.dtype, -1) for t in tensors]))
+
+
+def disco_grad_workspace_bytes(count: int) -> int:
+    return _lib.disco_grad_workspace_bytes(count)
+
+
+def disco_grad_norm(src, norm, workspace, workspace_bytes, accumulate=0, stream=None, check=True) -> int:
+    """`src`: a list of torch tensors, contiguous, fp32 or bf16."""
+    at, elements, dtypes = _listed(src)
+    st = _lib.disco_grad_norm(at, elements, dtypes, len(src), int(accumulate), _ptr(norm), _ptr(workspace), workspace_bytes, _stream_ptr(stream))
+    if check and st != DISCO_OK:
+        raise DiscoError(st, "disco_grad_norm")
+    return st
+
+
+def disco_grad_clip(src, dst, max_norm, given, norm, workspace, workspace_bytes, stream=None, check=True) -> int:
+    """`src`, `dst`: lists of torch tensors, contiguous, fp32 or bf16, of the same sizes and types; `dst` may be `src`."""
+    at, elements, dtypes = _listed(src)
+    to = at
+    if dst is not src:
+        to, n, types = _listed(dst)
+        if list(n) != list(elements) or list(types) != list(dtypes):
+            raise ValueError("dst has other sizes or types than src")
+    st = _lib.disco_grad_clip(at, to, elements, dtypes, len(src), max_norm, _ptr(given), _ptr(norm), _ptr(workspace), workspace_bytes,
+                              _stream_ptr(stream))
+    if check and st != DISCO_OK:
+        raise DiscoError(st, "disco_grad_clip")
     return st

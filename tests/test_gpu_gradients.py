@@ -1,0 +1,134 @@
+"""disco_grad_norm and disco_grad_clip against float64.  The norm is a float64 sum rounded once (2^-24); a clipped value is the gradient times a
+factor that carries the rounding of the norm, of norm + 1e-6, of the quotient and of itself times the gradient (4 of 2^-24), stored with half a step of its
+type (bf16 2^-8)."""
+import math
+
+import pytest
+import torch
+
+import paper_2304_08480_amd as dl
+
+pytestmark = pytest.mark.gpu
+STEP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+
+
+def _grads(sizes, seed=0, scale=1.0, types=(torch.float32, torch.bfloat16)):
+    g = torch.Generator().manual_seed(seed)
+    # every other one starts at an odd element
+    out = []
+    for i, n in enumerate(sizes):
+        t = (torch.randn(n + i % 2, generator=g) * scale).to(types[i % len(types)]).cuda()
+        out.append(t[i % 2:])
+    return out
+
+
+def _workspace(n):
+    need = dl.disco_grad_workspace_bytes(n)
+    return torch.full((need,), 255, dtype=torch.uint8, device="cuda"), need
+
+
+def _norm(grads):
+    return math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+
+
+def _check(grads, outs, max_norm, norm):
+    want = _norm(grads)
+    assert norm == pytest.approx(want, rel=2.0 ** -23)
+    factor = min(1.0, max_norm / (want + 1e-6))
+    for g, o in zip(grads, outs):
+        exact = g.double() * factor
+        bound = exact.abs() * (STEP[g.dtype] + 4 * 2.0 ** -24) + 1e-45
+        assert not g.numel() or float(((o.double() - exact).abs() - bound).max()) <= 0
+
+
+@pytest.mark.parametrize("sizes", [[1], [0, 7, 0, 8], [9, 8191, 8192, 8193], [100003, 3, 65536, 1], [5] * 500, [20_000_001, 17]], ids=lambda s: f"{len(s)}x{s[0]}")
+@pytest.mark.parametrize("max_norm", [0.5, 1e9])
+def test_sizes(sizes, max_norm):
+    print("case clip", len(sizes), sizes[0], max_norm, flush=True)
+    grads = _grads(sizes, seed=len(sizes))
+    before = [g.clone() for g in grads]
+    ws, need = _workspace(len(grads))
+    norm = torch.full((1,), float("nan"), device="cuda")
+    outs = [torch.full_like(g, float("nan")) for g in grads]
+    dl.disco_grad_clip(grads, outs, max_norm, None, norm, ws, need, torch.cuda.current_stream())
+    _check(before, outs, max_norm, float(norm))
+    assert all(torch.equal(a, b) for a, b in zip(grads, before))
+    only = torch.zeros(1, device="cuda")
+    dl.disco_grad_norm(grads, only, ws, need, stream=torch.cuda.current_stream())
+    assert torch.equal(only, norm)
+    dl.disco_grad_clip(grads, grads, max_norm, None, norm, ws, need, torch.cuda.current_stream())      # in place
+    assert all(torch.equal(a, b) for a, b in zip(grads, outs))
+
+
+def test_lists_in_parts_and_a_given_norm():
+    grads = _grads([1000, 33, 70000, 5], seed=2)
+    ws, need = _workspace(4)
+    norm = torch.zeros(1, device="cuda")
+    stream = torch.cuda.current_stream()
+    dl.disco_grad_norm(grads[:2], norm, ws, need, stream=stream)
+    dl.disco_grad_norm(grads[2:], norm, ws, need, accumulate=1, stream=stream)
+    assert float(norm) == pytest.approx(_norm(grads), rel=2.0 ** -22)
+    outs = [torch.empty_like(g) for g in grads]
+    kept = torch.zeros(1, device="cuda")
+    for part in (slice(0, 2), slice(2, 4)):
+        dl.disco_grad_clip(grads[part], outs[part], 2.0, norm, kept, ws, need, stream)
+    assert torch.equal(kept, norm)
+    for g, o in zip(grads, outs):
+        exact = g.double() * (2.0 / (float(norm) + 1e-6))
+        assert float(((o.double() - exact).abs() - exact.abs() * (STEP[g.dtype] + 4 * 2.0 ** -24)).max()) <= 0
+    dl.disco_grad_clip(grads, outs, 2.0, norm, norm, ws, need, stream)
+    assert torch.equal(kept, norm)
+
+
+def test_empty_lists():
+    ws, need = _workspace(0)
+    norm = torch.full((1,), 3.0, device="cuda")
+    dl.disco_grad_norm([], norm, ws, need, accumulate=1, stream=torch.cuda.current_stream())
+    assert float(norm) == 3.0
+    dl.disco_grad_clip([], [], 1.0, None, norm, ws, need, torch.cuda.current_stream())
+    assert float(norm) == 0.0
+
+
+@pytest.mark.parametrize("value", [1e30, 1e-30, 3e38])
+def test_squares_outside_fp32(value):
+    grads = [torch.full((1000,), value, device="cuda"), torch.full((24,), -value, device="cuda")]
+    ws, need = _workspace(2)
+    norm = torch.zeros(1, device="cuda")
+    dl.disco_grad_norm(grads, norm, ws, need, stream=torch.cuda.current_stream())
+    want = value * 32.0
+    assert float(norm) == (math.inf if want > 3.5e38 else pytest.approx(want, rel=1e-6))
+
+
+def test_not_finite():
+    ws, need = _workspace(2)
+    norm = torch.zeros(1, device="cuda")
+    for bad, want in ((float("inf"), 0.0), (float("nan"), math.nan)):
+        grads = _grads([100, 50], types=(torch.float32,))
+        grads[1][7] = bad
+        outs = [torch.empty_like(g) for g in grads]
+        dl.disco_grad_clip(grads, outs, 1.0, None, norm, ws, need, torch.cuda.current_stream())
+        assert math.isinf(float(norm)) if want == 0.0 else math.isnan(float(norm))
+        assert (outs[0] == 0).all() if want == 0.0 else torch.isnan(outs[0]).all()
+    grads = _grads([100, 50], types=(torch.float32,))
+    outs = [torch.empty_like(g) for g in grads]
+    dl.disco_grad_clip(grads, outs, math.inf, None, norm, ws, need, torch.cuda.current_stream())
+    assert all(torch.equal(a, b) for a, b in zip(grads, outs))
+
+
+def test_captured_and_equal_bits():
+    grads = _grads([50000, 3, 777, 128 * 128] * 60, seed=5)
+    ws, need = _workspace(len(grads))
+    norm = torch.zeros(1, device="cuda")
+    outs = [torch.empty_like(g) for g in grads]
+    dl.disco_grad_clip(grads, outs, 1.0, None, norm, ws, need, torch.cuda.current_stream())
+    want, size = [o.clone() for o in outs], norm.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dl.disco_grad_clip(grads, outs, 1.0, None, norm, ws, need, torch.cuda.current_stream())
+    for _ in range(3):
+        for o in outs:
+            o.fill_(float("nan"))
+        norm.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(norm, size) and all(torch.equal(a, b) for a, b in zip(outs, want))
