@@ -24,6 +24,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -88,19 +89,33 @@ struct Layout {
 };
 
 // ROWS rows of a matrix on their way to the LDS, through registers so that they are under way while the previous tile is used.  Rows
-// past `rows` and pieces past the head's width are zeros: they meet zeros or masked values, never what lies behind them.
+// past `rows` and pieces past the head's width are zeros, by the bounds of the buffer resource: they meet zeros or masked values, never what lies
+// behind them.
+constexpr uint32_t NOWHERE = 0xfffffff0u;       // past the end of any buffer
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const __bf16* base, int64_t pitch, int rows, int most, int head_dim) {
+  const uint64_t v = reinterpret_cast<uint64_t>(base);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  const uint32_t n = rows <= 0 ? 0 : rows < most ? rows : most;
+  const uint32_t bytes = n ? (n - 1) * (uint32_t)(pitch * 2) + (uint32_t)head_dim * 2 : 0;
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
 template <int DP, int ROWS, int THREADS>
 struct Stage {
   using L = Layout<DP>;
   static constexpr int ALL = ROWS * L::PIECES, N = (ALL + THREADS - 1) / THREADS;
   u32x4 v[N];
-  __device__ __forceinline__ void fetch(const __bf16* base, int64_t pitch, int rows, int head_dim) {
+  uint32_t from[N];
+  __device__ __forceinline__ void init(int64_t pitch, int head_dim) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int id = threadIdx.x + i * THREADS, row = id / L::PIECES, piece = id % L::PIECES;
-      v[i] = u32x4{0, 0, 0, 0};
-      if (row < rows && row < ROWS && piece * 8 < head_dim) v[i] = *reinterpret_cast<const u32x4*>(base + row * pitch + piece * 8);
+      from[i] = piece * 8 < head_dim && row < ROWS ? (uint32_t)row * (uint32_t)(pitch * 2) + piece * 16 : NOWHERE;
     }
+  }
+  __device__ __forceinline__ void fetch(const __bf16* base, int64_t pitch, int rows, int head_dim) {
+    const __amdgpu_buffer_rsrc_t r = rows_at(base, pitch, rows, ROWS, head_dim);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, from[i], 0, 0));
   }
   __device__ __forceinline__ void put(char* lds) const {
 #pragma unroll
@@ -134,54 +149,78 @@ __device__ __forceinline__ f32x16 zeros16() {
   return z;
 }
 
-// 32 walked rows from `row0` on times the lanes' rows: element r of a lane is walked row row0 + 8 (r / 4) + 4 half + r % 4.
-template <int DP>
-__device__ __forceinline__ f32x16 products(const char* lds, int row0, const Rows<DP>& b) {
+// 32 walked rows times the lanes' rows: element r of a lane is walked row 8 (r / 4) + 4 half + r % 4.  N such products at once, c[n] of
+// the rows at lds + n STEP with b(n, s): they share the addresses, and no product waits for the one before it.  (The lane's address is hidden from the
+// compiler: it would keep one register for each of the DP / 16 pieces, 16 more in accumulate(), and have none left for two waves a SIMD.)
+template <int DP, int N, int STEP, class B>
+__device__ __forceinline__ void products(f32x16 (&c)[N], const char* lds, B b) {
   using L = Layout<DP>;
-  const int lane = threadIdx.x & 63, row = row0 + (lane & 31), half = lane >> 5;
-  f32x16 c = zeros16();
+  const int lane = threadIdx.x & 63;
+  int base = L::at(lane & 31, lane >> 5);
+  asm volatile("" : "+v"(base));
 #pragma unroll
-  for (int s = 0; s < DP / 16; ++s) c = mfma(*reinterpret_cast<const bf16x8*>(lds + L::at(row, 2 * s + half)), b.f[s], c);
-  return c;
+  for (int s = 0; s < DP / 16; ++s) {
+    const char* at = lds + (base ^ s << 5);
+#pragma unroll
+    for (int n = 0; n < N; ++n) c[n] = mfma(*reinterpret_cast<const bf16x8*>(at + n * STEP), b(n, s, base), s ? c[n] : zeros16());
+  }
 }
 __device__ __forceinline__ int walked(int r, int half) { return 8 * (r >> 2) + 4 * half + (r & 3); }
 
-// acc[m] += (channels 32 m .. of the 32 walked rows, transposed) x (p: the lanes' values for those rows, in the order of products())
-template <int DP>
-__device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const char* lds, int row0, const f32x16& p) {
+// A lane's values for 32 walked rows as the B operand of two products over 16 of them each, in the order of products().
+struct Weights { bf16x8 f[2]; };
+__device__ __forceinline__ Weights rounded(const f32x16& p) {
+  Weights w;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w.f[j][e] = (__bf16)p[8 * j + e];
+  return w;
+}
+// acc_n[m] += (channels 32 m .. of 32 walked rows at lds + n STEP, transposed) x weights_n, N of them with shared addresses
+template <int DP, int N, int STEP>
+__device__ __forceinline__ void accumulate(f32x16 (*const (&acc)[N])[DP / 32], const char* lds, const Weights (&w)[N]) {
   using L = Layout<DP>;
   const int lane = threadIdx.x & 63, half = lane >> 5, in16 = lane & 15, high = lane >> 4 & 1;
+  int base = L::at(4 * half + (in16 >> 2), 2 * high + ((in16 & 3) >> 1)) + 8 * (in16 & 1);
+  asm volatile("" : "+v"(base));
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    bf16x8 b;
+  for (int m = 0; m < DP / 32; ++m) {
+    // 8 rows on, the swizzle has bit 1 of the piece the other way round
+    const char *even = lds + (base ^ m << 6), *odd = lds + 8 * L::PITCH + (base ^ (m << 6 | 32));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) b[e] = (__bf16)p[8 * j + e];
-    const int row = row0 + 16 * j + 4 * half + (in16 >> 2);
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int m = 0; m < DP / 32; ++m) {
-      const int piece = 4 * m + 2 * high + ((in16 & 3) >> 1), byte = 8 * (in16 & 1);
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + L::at(row, piece) + byte));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + L::at(row + 8, piece) + byte));
-      acc[m] = mfma(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), b, acc[m]);
-    }
+      for (int n = 0; n < N; ++n) {
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(even + 16 * j * L::PITCH + n * STEP));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(odd + 16 * j * L::PITCH + n * STEP));
+        (*acc[n])[m] = mfma(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), w[n].f[j], (*acc[n])[m]);
+      }
   }
 }
 
-// A lane's row of an accumulated product, times f, as bf16: 4 consecutive channels a store.
+// A lane's row of an accumulated product, times f, as bf16.  The two halves of a wave hold 4 channels each of every 8 of a row: they exchange
+// them, so that each stores 8.
 template <int DP>
-__device__ __forceinline__ void store_row(__bf16* row, const f32x16 (&acc)[DP / 32], float f, int head_dim) {
+__device__ __forceinline__ void store_row(__bf16* row, const f32x16 (&acc)[DP / 32], float f, int head_dim, bool there) {
   const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
   for (int m = 0; m < DP / 32; ++m)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int c = 32 * m + 8 * g + 4 * half;
-      if (c < head_dim) {
-        bf16x4 w;
+    for (int g = 0; g < 4; g += 2) {
+      u32x4 w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (__bf16)(acc[m][4 * g + e] * f);
-        *reinterpret_cast<bf16x4*>(row + c) = w;
+      for (int e = 0; e < 2; ++e) {
+        const auto pack = [&](int r) {
+          const bf16x2 v = {(__bf16)(acc[m][r] * f), (__bf16)(acc[m][r + 1] * f)};
+          return __builtin_bit_cast(uint32_t, v);
+        };
+        const auto x = __builtin_amdgcn_permlane32_swap(pack(4 * g + 2 * e), pack(4 * g + 4 + 2 * e), false, false);
+        w[e] = x[0];
+        w[2 + e] = x[1];
       }
+      const int c = 32 * m + 8 * (g + half);
+      if (there && c < head_dim) *reinterpret_cast<u32x4*>(row + c) = w;
     }
 }
 
@@ -191,90 +230,130 @@ template <int DP, int WAVES>
 struct Shape {
   static constexpr int THREADS = 64 * WAVES, OWN = 32 * WAVES;      // rows of the side in registers
   static constexpr int WALK = WAVES == 1 ? 32 : 64;                 // rows of a walked tile
-  static constexpr int TILE = WALK * Layout<DP>::PITCH;
+  static constexpr int SUB = 32 * Layout<DP>::PITCH, TILE = WALK * Layout<DP>::PITCH;
+};
+
+// A wave's share of the forward pass: 32 queries, one a lane, the keys walked.
+template <int DP>
+struct Forward {
+  Rows<DP> q;
+  f32x16 acc[DP / 32];
+  float top = -INFINITY, total = 0.f;            // the lane's reference (not always its maximum) and its half's sum
+  // SUBS times 32 keys from key j on; keys past `last` are masked where `edge`
+  template <int SUBS>
+  __device__ __forceinline__ void step(const char* lds_k, const char* lds_v, int j, bool edge, int last, float c) {
+    constexpr int SUB = 32 * Layout<DP>::PITCH;
+    const int half = (threadIdx.x & 63) >> 5;
+    f32x16 s[SUBS];
+    products<DP, SUBS, SUB>(s, lds_k, [&](int, int k, int) { return q.f[k]; });
+    if (edge) {
+      const int most = last - j - 4 * half;
+#pragma unroll
+      for (int n = 0; n < SUBS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * n + walked(r, 0) > most) s[n][r] = -INFINITY;
+    }
+    float m = s[0][0];
+#pragma unroll
+    for (int n = 0; n < SUBS; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) m = fmaxf(m, s[n][r]);
+    m = fmaxf(m, other_half(m));
+    // The reference follows the maximum only when a row's has risen by 2^8 since: sums stay below 2^8 times their number of terms, bf16 values keep their
+    // relative precision, and the accumulators are rescaled a few times a row instead of at every step.
+    if (__any((m - top) * c > 8.f)) {
+      const float next = fmaxf(top, m), fade = __builtin_amdgcn_exp2f((top - next) * c);
+      top = next;
+      total *= fade;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) acc[d] *= fade;
+    }
+    const float ref = top * c;
+    float sum[2] = {0.f, 0.f};
+    Weights w[SUBS];
+#pragma unroll
+    for (int n = 0; n < SUBS; ++n) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], c, -ref));
+        sum[r & 1] += s[n][r];
+      }
+      w[n] = rounded(s[n]);
+    }
+    total += sum[0] + sum[1];
+#pragma unroll
+    for (int n = 0; n < SUBS; ++n) accumulate<DP, 1, 0>({&acc}, lds_v + n * SUB, {w[n]});
+  }
 };
 
 template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_attention_fwd(Args a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attention_fwd(Args a) {
   using S = Shape<DP, WAVES>;
-  __shared__ __attribute__((aligned(16))) char lds_k[S::TILE];
-  __shared__ __attribute__((aligned(16))) char lds_v[S::TILE];
+  __shared__ __attribute__((aligned(16))) char lds[4 * S::TILE];        // keys and values, two tiles in turn
   const int head = blockIdx.x % a.heads;
   Tile t;
   if (!find_tile<S::OWN>(a, a.slots - 1 - (int)(blockIdx.x / a.heads), t)) return;
   const int kv = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, half = lane >> 5;
   const int first = t.row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
-  Rows<DP> q;
-  q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, mine < t.len, a.head_dim);
   const __bf16* k = a.k + t.first * a.k_row + kv * a.k_head;
   const __bf16* v = a.v + t.first * a.v_row + kv * a.v_head;
-  const int end = a.causal && t.row + S::OWN < t.len ? t.row + S::OWN : t.len;      // keys that the workgroup sees
-  const int seen = a.causal && first + 32 < t.len ? first + 32 : t.len;             // and this wave
-  const int last = a.causal && mine < t.len ? mine : t.len - 1;                     // the lane's last key
-  const float c = a.scale * LOG2E;
-  float top = -INFINITY, total = 0.f;
-  f32x16 acc[DP / 32];
-#pragma unroll
-  for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
   Stage<DP, S::WALK, S::THREADS> sk, sv;
+  sk.init(a.k_row, a.head_dim);
+  sv.init(a.v_row, a.head_dim);
   sk.fetch(k, a.k_row, t.len, a.head_dim);
   sv.fetch(v, a.v_row, t.len, a.head_dim);
-  for (int j0 = 0; j0 < end; j0 += S::WALK) {
-    __syncthreads();
-    sk.put(lds_k);
-    sv.put(lds_v);
-    __syncthreads();
-    if (j0 + S::WALK < end) {
-      sk.fetch(k + (int64_t)(j0 + S::WALK) * a.k_row, a.k_row, t.len - j0 - S::WALK, a.head_dim);
-      sv.fetch(v + (int64_t)(j0 + S::WALK) * a.v_row, a.v_row, t.len - j0 - S::WALK, a.head_dim);
+  Forward<DP> f;
+  f.q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, mine < t.len, a.head_dim);
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m) f.acc[m] = zeros16();
+  const int end = a.causal && t.row + S::OWN < t.len ? t.row + S::OWN : t.len;      // keys that the workgroup sees
+  const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;      // and this wave
+  const int last = a.causal && mine < t.len ? mine : t.len - 1;                     // the lane's last key
+  const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;              // keys before this one need no mask
+  const float c = a.scale * LOG2E;
+  sk.put(lds);
+  sv.put(lds + S::TILE);
+  __syncthreads();
+  for (int j = 0, turn = 0; j < end; j += S::WALK, turn ^= 2 * S::TILE) {
+    const bool more = j + S::WALK < end;
+    if (more) {
+      sk.fetch(k + (int64_t)(j + S::WALK) * a.k_row, a.k_row, t.len - j - S::WALK, a.head_dim);
+      sv.fetch(v + (int64_t)(j + S::WALK) * a.v_row, a.v_row, t.len - j - S::WALK, a.head_dim);
     }
-#pragma unroll
-    for (int sub = 0; sub < S::WALK; sub += 32) {
-      const int j = j0 + sub;
-      if (j >= seen || first >= t.len) break;
-      f32x16 s = products<DP>(lds_k, sub, q);
-      if (j + 31 > first || j + 31 >= t.len) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (j + walked(r, half) > last) s[r] = -INFINITY;
-      }
-      float m = s[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) m = fmaxf(m, s[r]);
-      m = fmaxf(top, fmaxf(m, other_half(m)));
-      const float fade = __builtin_amdgcn_exp2f((top - m) * c), ref = m * c;
-      top = m;
-      float sum = 0.f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -ref));
-        sum += s[r];
-      }
-      total = fmaf(total, fade, sum);
-#pragma unroll
-      for (int m2 = 0; m2 < DP / 32; ++m2) acc[m2] *= fade;
-      accumulate<DP>(acc, lds_v, sub, s);
+    const char *lds_k = lds + turn, *lds_v = lds_k + S::TILE;
+    if (S::WALK > 32 && j + 32 < seen) f.template step<S::WALK / 32>(lds_k, lds_v, j, j + S::WALK > whole, last, c);
+    else if (j < seen) f.template step<1>(lds_k, lds_v, j, j + 32 > whole, last, c);
+    if (more) {
+      sk.put(lds + (turn ^ 2 * S::TILE));
+      sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
     }
+    __syncthreads();
   }
-  total += other_half(total);
-  if (mine < t.len) {
-    store_row<DP>(a.out + (t.first + mine) * a.o_row + head * a.o_head, acc, 1.f / total, a.head_dim);
-    if (half == 0) a.lse[head * a.tokens + t.first + mine] = top * a.scale + __builtin_amdgcn_logf(total) * LN2;
-  }
+  f.total += other_half(f.total);
+  const bool there = mine < t.len;
+  store_row<DP>(a.out + (t.first + mine) * a.o_row + head * a.o_head, f.acc, 1.f / f.total, a.head_dim, there);
+  if (there && half == 0) a.lse[head * a.tokens + t.first + mine] = f.top * a.scale + __builtin_amdgcn_logf(f.total) * LN2;
 }
 
 // dq, and delta = <do, o> of every row for the kernel of dk and dv, which runs after this one.
 template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_attention_bwd_q(Args a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attention_bwd_q(Args a) {
   using S = Shape<DP, WAVES>;
-  __shared__ __attribute__((aligned(16))) char lds_k[S::TILE];
-  __shared__ __attribute__((aligned(16))) char lds_v[S::TILE];
+  __shared__ __attribute__((aligned(16))) char lds[4 * S::TILE];
   const int head = blockIdx.x % a.heads;
   Tile t;
   if (!find_tile<S::OWN>(a, a.slots - 1 - (int)(blockIdx.x / a.heads), t)) return;
   const int kv = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, half = lane >> 5;
   const int first = t.row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
   const bool there = mine < t.len;
+  const __bf16* k = a.k + t.first * a.k_row + kv * a.k_head;
+  const __bf16* v = a.v + t.first * a.v_row + kv * a.v_head;
+  Stage<DP, S::WALK, S::THREADS> sk, sv;
+  sk.init(a.k_row, a.head_dim);
+  sv.init(a.v_row, a.head_dim);
+  sk.fetch(k, a.k_row, t.len, a.head_dim);
+  sv.fetch(v, a.v_row, t.len, a.head_dim);
   Rows<DP> q, dout;
   q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, there, a.head_dim);
   dout.fetch(a.dout + (t.first + mine) * a.o_row + head * a.o_head, there, a.head_dim);
@@ -291,117 +370,147 @@ __global__ __launch_bounds__(64 * WAVES) void k_attention_bwd_q(Args a) {
   const int64_t at = head * a.tokens + t.first + mine;
   if (there && half == 0) a.delta[at] = delta;
   const float lse2 = there ? a.lse[at] * LOG2E : 0.f;
-  const __bf16* k = a.k + t.first * a.k_row + kv * a.k_head;
-  const __bf16* v = a.v + t.first * a.v_row + kv * a.v_head;
   const int end = a.causal && t.row + S::OWN < t.len ? t.row + S::OWN : t.len;
-  const int seen = a.causal && first + 32 < t.len ? first + 32 : t.len;
-  const int last = a.causal && mine < t.len ? mine : t.len - 1;
+  const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;
+  const int last = a.causal && there ? mine : t.len - 1;
+  const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;
   const float c = a.scale * LOG2E;
   f32x16 acc[DP / 32];
 #pragma unroll
   for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
-  Stage<DP, S::WALK, S::THREADS> sk, sv;
-  sk.fetch(k, a.k_row, t.len, a.head_dim);
-  sv.fetch(v, a.v_row, t.len, a.head_dim);
-  for (int j0 = 0; j0 < end; j0 += S::WALK) {
-    __syncthreads();
-    sk.put(lds_k);
-    sv.put(lds_v);
-    __syncthreads();
-    if (j0 + S::WALK < end) {
+  sk.put(lds);
+  sv.put(lds + S::TILE);
+  __syncthreads();
+  for (int j0 = 0, turn = 0; j0 < end; j0 += S::WALK, turn ^= 2 * S::TILE) {
+    const bool more = j0 + S::WALK < end;
+    if (more) {
       sk.fetch(k + (int64_t)(j0 + S::WALK) * a.k_row, a.k_row, t.len - j0 - S::WALK, a.head_dim);
       sv.fetch(v + (int64_t)(j0 + S::WALK) * a.v_row, a.v_row, t.len - j0 - S::WALK, a.head_dim);
     }
 #pragma unroll
     for (int sub = 0; sub < S::WALK; sub += 32) {
       const int j = j0 + sub;
-      if (j >= seen || first >= t.len) break;
-      f32x16 s = products<DP>(lds_k, sub, q);
-      const f32x16 dp = products<DP>(lds_v, sub, dout);
-      const bool edge = j + 31 > first || j + 31 >= t.len;
+      if (j >= seen) break;
+      const char* lds_k = lds + turn + sub * Layout<DP>::PITCH;
+      f32x16 s[2];                                                  // scores, and dP
+      products<DP, 2, S::TILE>(s, lds_k, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
+      if (j + 32 > whole) {
+        const int most = last - j - 4 * half;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2));
-        s[r] = edge && j + walked(r, half) > last ? 0.f : p * (dp[r] - delta);
+        for (int r = 0; r < 16; ++r)
+          if (walked(r, 0) > most) s[0][r] = -INFINITY;
       }
-      accumulate<DP>(acc, lds_k, sub, s);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2)) * (s[1][r] - delta);
+      accumulate<DP, 1, 0>({&acc}, lds_k, {rounded(s[0])});
     }
+    if (more) {
+      sk.put(lds + (turn ^ 2 * S::TILE));
+      sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
+    }
+    __syncthreads();
   }
-  if (there) store_row<DP>(a.dq + (t.first + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim);
+  store_row<DP>(a.dq + (t.first + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, there);
 }
 
 // dk and dv: 32 keys a wave; the queries of all heads that share the keys are walked, head by head.
 template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_attention_bwd_kv(Args a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attention_bwd_kv(Args a) {
   using S = Shape<DP, WAVES>;
-  constexpr int WALK = 32;
-  __shared__ __attribute__((aligned(16))) char lds_q[WALK * Layout<DP>::PITCH];
-  __shared__ __attribute__((aligned(16))) char lds_o[WALK * Layout<DP>::PITCH];
-  __shared__ __attribute__((aligned(16))) float row_lse[WALK], row_delta[WALK];
+  constexpr int WALK = 32, TILE = S::SUB, BOTH = 2 * TILE + 2 * WALK * (int)sizeof(float);      // queries, do, lse, delta
+  // Wide heads: the accumulators of dk and dv take 2 DP registers a lane, k and v another DP; with v in the LDS two waves fit a SIMD.
+  constexpr bool V_IN_LDS = DP > 64;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BOTH];
+  __shared__ __attribute__((aligned(16))) char lds_v[V_IN_LDS ? S::OWN * Layout<DP>::PITCH : 16];
   const int kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads;
   Tile t;
-  if (!find_tile<S::OWN>(a, (int)(blockIdx.x / a.kv_heads), t)) return;
+  // Causal: the first key tiles have the most queries.  The order is first, second, ..., middle, last, last but one, ...: workgroups half the
+  // grid apart, which share a compute unit where all of them fit the chip at once, have equal work together.
+  const int order = blockIdx.x / a.kv_heads, upper = (a.slots + 1) / 2;
+  if (!find_tile<S::OWN>(a, order < upper ? order : a.slots - 1 - (order - upper), t)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int first = t.row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
   const bool there = mine < t.len;
-  Rows<DP> k, v;
-  k.fetch(a.k + (t.first + mine) * a.k_row + kv * a.k_head, there, a.head_dim);
-  v.fetch(a.v + (t.first + mine) * a.v_row + kv * a.v_head, there, a.head_dim);
   const float c = a.scale * LOG2E;
-  const int begin = a.causal ? t.row / WALK * WALK : 0;            // the first walked query that sees a key of the tile
-  const int tiles = (t.len - begin + WALK - 1) / WALK, all = tiles * group;
-  f32x16 dk[DP / 32], dv[DP / 32];
-#pragma unroll
-  for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
+  const int begin = a.causal ? t.row : 0;                          // the first walked query (t.row is a multiple of 32)
+  const int tiles = (t.len - begin + WALK - 1) / WALK;
   Stage<DP, WALK, S::THREADS> sq, so;
+  sq.init(a.q_row, a.head_dim);
+  so.init(a.o_row, a.head_dim);
   float next_lse = 0.f, next_delta = 0.f;
-  auto fetch = [&](int n) {
-    const int head = kv * group + n / tiles, i0 = begin + n % tiles * WALK;
-    const int64_t row = t.first + i0;
-    sq.fetch(a.q + row * a.q_row + head * a.q_head, a.q_row, t.len - i0, a.head_dim);
-    so.fetch(a.dout + row * a.o_row + head * a.o_head, a.o_row, t.len - i0, a.head_dim);
+  int head = kv * group, i = begin;                                // what is fetched next
+  auto fetch = [&] {
+    const int64_t row = t.first + i;
+    sq.fetch(a.q + row * a.q_row + head * a.q_head, a.q_row, t.len - i, a.head_dim);
+    so.fetch(a.dout + row * a.o_row + head * a.o_head, a.o_row, t.len - i, a.head_dim);
     if (threadIdx.x < WALK) {
       // rows past the last: exp2(-inf) = 0
-      const bool row_there = i0 + (int)threadIdx.x < t.len;
+      const bool row_there = i + (int)threadIdx.x < t.len;
       const int64_t at = head * a.tokens + row + threadIdx.x;
       next_lse = row_there ? a.lse[at] * LOG2E : INFINITY;
       next_delta = row_there ? a.delta[at] : 0.f;
     }
+    i += WALK;
+    if (i >= t.len) { i = begin; ++head; }
   };
-  fetch(0);
-  for (int n = 0; n < all; ++n) {
-    const int i = begin + n % tiles * WALK;
-    __syncthreads();
-    sq.put(lds_q);
-    so.put(lds_o);
+  auto put = [&](char* to) {
+    sq.put(to);
+    so.put(to + TILE);
     if (threadIdx.x < WALK) {
-      row_lse[threadIdx.x] = next_lse;
-      row_delta[threadIdx.x] = next_delta;
+      reinterpret_cast<float*>(to + 2 * TILE)[threadIdx.x] = next_lse;
+      reinterpret_cast<float*>(to + 2 * TILE)[WALK + threadIdx.x] = next_delta;
     }
-    __syncthreads();
-    if (n + 1 < all) fetch(n + 1);
-    if (first >= t.len || (a.causal && i + WALK <= first)) continue;
-    f32x16 s = products<DP>(lds_q, 0, k);
-    f32x16 dp = products<DP>(lds_o, 0, v);
-    const bool edge = a.causal && i < first + 31;
+  };
+  fetch();
+  char* const own_v = lds_v + S::SUB * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Rows<DP> k, v;
+  k.fetch(a.k + (t.first + mine) * a.k_row + kv * a.k_head, there, a.head_dim);
+  v.fetch(a.v + (t.first + mine) * a.v_row + kv * a.v_head, there, a.head_dim);
+  if (V_IN_LDS) {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4 l = *reinterpret_cast<const f32x4*>(row_lse + 8 * g + 4 * half), d = *reinterpret_cast<const f32x4*>(row_delta + 8 * g + 4 * half);
+    for (int s = 0; s < DP / 16; ++s) *reinterpret_cast<bf16x8*>(own_v + Layout<DP>::at(lane & 31, 2 * s + half)) = v.f[s];
+  }
+  f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = 4 * g + e;
-        const float p = edge && i + walked(r, half) < mine ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[e]));
-        dp[r] = edge && i + walked(r, half) < mine ? 0.f : p * (dp[r] - d[e]);
-        s[r] = p;
+  for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
+  put(lds);
+  __syncthreads();
+  int at = begin;                                                  // what is used now
+  for (int n = tiles * group, turn = 0; n > 0; --n, turn ^= 1) {
+    char* const now = lds + turn * BOTH;
+    if (n > 1) fetch();
+    if (first < t.len && !(a.causal && at + WALK <= first)) {
+      f32x16 s[2];                                                  // scores, and dP
+      products<DP, 2, TILE>(s, now, [&](int which, int p, int base) {
+        if (!which) return k.f[p];
+        return V_IN_LDS ? *reinterpret_cast<const bf16x8*>(own_v + (base ^ p << 5)) : v.f[p];
+      });
+      if (a.causal && at < first + 31) {
+        const int least = mine - at - 4 * half;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (walked(r, 0) < least) s[0][r] = -INFINITY;
       }
+      const float* scalars = reinterpret_cast<const float*>(now + 2 * TILE) + 4 * half;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 l = *reinterpret_cast<const f32x4*>(scalars + 8 * g), d = *reinterpret_cast<const f32x4*>(scalars + WALK + 8 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * g + e;
+          s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
+          s[1][r] = s[0][r] * (s[1][r] - d[e]);
+        }
+      }
+      accumulate<DP, 2, TILE>({&dk, &dv}, now, {rounded(s[1]), rounded(s[0])});
     }
-    accumulate<DP>(dv, lds_o, 0, s);
-    accumulate<DP>(dk, lds_q, 0, dp);
+    at += WALK;
+    if (at >= t.len) at = begin;
+    if (n > 1) put(lds + (turn ^ 1) * BOTH);
+    __syncthreads();
   }
-  if (there) {
-    store_row<DP>(a.dk + (t.first + mine) * a.k_row + kv * a.k_head, dk, a.scale, a.head_dim);
-    store_row<DP>(a.dv + (t.first + mine) * a.v_row + kv * a.v_head, dv, 1.f, a.head_dim);
-  }
+  store_row<DP>(a.dk + (t.first + mine) * a.k_row + kv * a.k_head, dk, a.scale, a.head_dim, there);
+  store_row<DP>(a.dv + (t.first + mine) * a.v_row + kv * a.v_head, dv, 1.f, a.head_dim, there);
 }
 
 int check(const disco_attention_shape* s) {
@@ -412,9 +521,13 @@ int check(const disco_attention_shape* s) {
   // what one launch of 32-row tiles has workgroups for
   if ((s->tokens / 32 + s->sequences) * s->heads > 0x7fffffff) return DISCO_ERR_SHAPE;
   if (s->dtype != DISCO_BF16 || s->head_dim % 8 != 0 || s->head_dim > 128) return DISCO_ERR_UNSUPPORTED;
-  const int64_t strides[] = {s->q_row, s->q_head, s->k_row, s->k_head, s->v_row, s->v_head, s->o_row, s->o_head};
-  for (int64_t v : strides) {
-    if (v <= 0 || v > (int64_t)1 << 31) return DISCO_ERR_SHAPE;
+  // the 64 rows of a tile are addressed with 32 bits
+  for (int64_t v : {s->q_row, s->k_row, s->v_row, s->o_row}) {
+    if (v <= 0 || v > (int64_t)1 << 24) return DISCO_ERR_SHAPE;
+    if (v % 8 != 0) return DISCO_ERR_UNSUPPORTED;
+  }
+  for (int64_t v : {s->q_head, s->k_head, s->v_head, s->o_head}) {
+    if (v <= 0 || v > (int64_t)1 << 40) return DISCO_ERR_SHAPE;
     if (v % 8 != 0) return DISCO_ERR_UNSUPPORTED;
   }
   return DISCO_OK;
