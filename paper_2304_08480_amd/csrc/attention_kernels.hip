@@ -47,7 +47,10 @@ struct Args {
 // Which tile of T rows of which sequence a workgroup has.  Sequence s owns the slots from starts[s] / T + s on: at least as many as it has
 // tiles, whatever its start, so the tiles are found with no table and no count of them, for at most `sequences` idle workgroups more.  The
 // search is 64 ways wide: two rounds of loads for thousands of sequences.  What it reads is kept within [0, tokens].
-struct Tile { int64_t first; int32_t len, row; };        // the sequence's first row and length, the tile's first row in it
+//
+// Causal: the later a tile of queries (the earlier a tile of keys), the more it has to do.  A workgroup takes a tile and the one that lies as far
+// from the sequence's other end, so that all of a sequence's workgroups have the same work.
+struct Tile { int64_t first; int32_t len, index, other; };        // the sequence's first row and length; index <= other, equal: one tile
 template <int T>
 __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
   const int lane = threadIdx.x & 63, tokens = (int)a.tokens;
@@ -67,9 +70,10 @@ __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
   const int from = start(lo), to = start(lo + 1);
   t.first = __builtin_amdgcn_readfirstlane(from);
   t.len = __builtin_amdgcn_readfirstlane(to - from);
-  t.row = (slot - (from / T + lo)) * T;
-  t.row = __builtin_amdgcn_readfirstlane(t.row);
-  return t.row < t.len;
+  t.index = __builtin_amdgcn_readfirstlane(slot - (from / T + lo));
+  const int count = (t.len + T - 1) / T;
+  t.other = a.causal ? count - 1 - t.index : t.index;
+  return t.index < count && t.index <= t.other;
 }
 
 // A walked tile in the LDS: rows of DP elements, padded to a power of two of bytes, 16-byte pieces XOR-ed with bits of the row so that
@@ -247,7 +251,8 @@ struct Forward {
     f32x16 s[SUBS];
     products<DP, SUBS, SUB>(s, lds_k, [&](int, int k, int) { return q.f[k]; });
     if (edge) {
-      const int most = last - j - 4 * half;
+      int most = last - j - 4 * half;
+      asm volatile("" : "+v"(most));             // keeps the branch: as selects every tile would pay for it
 #pragma unroll
       for (int n = 0; n < SUBS; ++n)
 #pragma unroll
@@ -293,47 +298,51 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attention_fwd(Args a) {
   __shared__ __attribute__((aligned(16))) char lds[4 * S::TILE];        // keys and values, two tiles in turn
   const int head = blockIdx.x % a.heads;
   Tile t;
-  if (!find_tile<S::OWN>(a, a.slots - 1 - (int)(blockIdx.x / a.heads), t)) return;
+  if (!find_tile<S::OWN>(a, blockIdx.x / a.heads, t)) return;
   const int kv = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, half = lane >> 5;
-  const int first = t.row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
   const __bf16* k = a.k + t.first * a.k_row + kv * a.k_head;
   const __bf16* v = a.v + t.first * a.v_row + kv * a.v_head;
+  const float c = a.scale * LOG2E;
   Stage<DP, S::WALK, S::THREADS> sk, sv;
   sk.init(a.k_row, a.head_dim);
   sv.init(a.v_row, a.head_dim);
-  sk.fetch(k, a.k_row, t.len, a.head_dim);
-  sv.fetch(v, a.v_row, t.len, a.head_dim);
-  Forward<DP> f;
-  f.q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, mine < t.len, a.head_dim);
+#pragma nounroll
+  for (int tile = t.other;; tile = t.index) {
+    const int row = tile * S::OWN;
+    const int first = row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
+    sk.fetch(k, a.k_row, t.len, a.head_dim);
+    sv.fetch(v, a.v_row, t.len, a.head_dim);
+    Forward<DP> f;
+    f.q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, mine < t.len, a.head_dim);
 #pragma unroll
-  for (int m = 0; m < DP / 32; ++m) f.acc[m] = zeros16();
-  const int end = a.causal && t.row + S::OWN < t.len ? t.row + S::OWN : t.len;      // keys that the workgroup sees
-  const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;      // and this wave
-  const int last = a.causal && mine < t.len ? mine : t.len - 1;                     // the lane's last key
-  const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;              // keys before this one need no mask
-  const float c = a.scale * LOG2E;
-  sk.put(lds);
-  sv.put(lds + S::TILE);
-  __syncthreads();
-  for (int j = 0, turn = 0; j < end; j += S::WALK, turn ^= 2 * S::TILE) {
-    const bool more = j + S::WALK < end;
-    if (more) {
-      sk.fetch(k + (int64_t)(j + S::WALK) * a.k_row, a.k_row, t.len - j - S::WALK, a.head_dim);
-      sv.fetch(v + (int64_t)(j + S::WALK) * a.v_row, a.v_row, t.len - j - S::WALK, a.head_dim);
-    }
-    const char *lds_k = lds + turn, *lds_v = lds_k + S::TILE;
-    if (S::WALK > 32 && j + 32 < seen) f.template step<S::WALK / 32>(lds_k, lds_v, j, j + S::WALK > whole, last, c);
-    else if (j < seen) f.template step<1>(lds_k, lds_v, j, j + 32 > whole, last, c);
-    if (more) {
-      sk.put(lds + (turn ^ 2 * S::TILE));
-      sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
-    }
+    for (int m = 0; m < DP / 32; ++m) f.acc[m] = zeros16();
+    const int end = a.causal && row + S::OWN < t.len ? row + S::OWN : t.len;          // keys that the workgroup sees
+    const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;      // and this wave
+    const int last = a.causal && mine < t.len ? mine : t.len - 1;                     // the lane's last key
+    const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;              // keys before this one need no mask
+    sk.put(lds);
+    sv.put(lds + S::TILE);
     __syncthreads();
+    for (int j = 0, turn = 0; j < end; j += S::WALK, turn ^= 2 * S::TILE) {
+      const bool more = j + S::WALK < end;
+      if (more) {
+        sk.fetch(k + (int64_t)(j + S::WALK) * a.k_row, a.k_row, t.len - j - S::WALK, a.head_dim);
+        sv.fetch(v + (int64_t)(j + S::WALK) * a.v_row, a.v_row, t.len - j - S::WALK, a.head_dim);
+      }
+      const char *lds_k = lds + turn, *lds_v = lds_k + S::TILE;
+      if (j < seen) f.template step<S::WALK / 32>(lds_k, lds_v, j, j + S::WALK > whole, last, c);
+      if (more) {
+        sk.put(lds + (turn ^ 2 * S::TILE));
+        sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
+      }
+      __syncthreads();
+    }
+    f.total += other_half(f.total);
+    const bool there = mine < t.len;
+    store_row<DP>(a.out + (t.first + mine) * a.o_row + head * a.o_head, f.acc, 1.f / f.total, a.head_dim, there);
+    if (there && half == 0) a.lse[head * a.tokens + t.first + mine] = f.top * a.scale + __builtin_amdgcn_logf(f.total) * LN2;
+    if (tile == t.index) break;
   }
-  f.total += other_half(f.total);
-  const bool there = mine < t.len;
-  store_row<DP>(a.out + (t.first + mine) * a.o_row + head * a.o_head, f.acc, 1.f / f.total, a.head_dim, there);
-  if (there && half == 0) a.lse[head * a.tokens + t.first + mine] = f.top * a.scale + __builtin_amdgcn_logf(f.total) * LN2;
 }
 
 // dq, and delta = <do, o> of every row for the kernel of dk and dv, which runs after this one.
@@ -343,174 +352,218 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attention_bwd_q(Args a) {
   __shared__ __attribute__((aligned(16))) char lds[4 * S::TILE];
   const int head = blockIdx.x % a.heads;
   Tile t;
-  if (!find_tile<S::OWN>(a, a.slots - 1 - (int)(blockIdx.x / a.heads), t)) return;
+  if (!find_tile<S::OWN>(a, blockIdx.x / a.heads, t)) return;
   const int kv = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, half = lane >> 5;
-  const int first = t.row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
-  const bool there = mine < t.len;
   const __bf16* k = a.k + t.first * a.k_row + kv * a.k_head;
   const __bf16* v = a.v + t.first * a.v_row + kv * a.v_head;
+  const float c = a.scale * LOG2E;
   Stage<DP, S::WALK, S::THREADS> sk, sv;
   sk.init(a.k_row, a.head_dim);
   sv.init(a.v_row, a.head_dim);
-  sk.fetch(k, a.k_row, t.len, a.head_dim);
-  sv.fetch(v, a.v_row, t.len, a.head_dim);
-  Rows<DP> q, dout;
-  q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, there, a.head_dim);
-  dout.fetch(a.dout + (t.first + mine) * a.o_row + head * a.o_head, there, a.head_dim);
-  float delta = 0.f;
-  {
-    Rows<DP> o;
-    o.fetch(a.o + (t.first + mine) * a.o_row + head * a.o_head, there, a.head_dim);
+#pragma nounroll
+  for (int tile = t.other;; tile = t.index) {
+    const int row = tile * S::OWN;
+    const int first = row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
+    const bool there = mine < t.len;
+    sk.fetch(k, a.k_row, t.len, a.head_dim);
+    sv.fetch(v, a.v_row, t.len, a.head_dim);
+    Rows<DP> q, dout;
+    q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, there, a.head_dim);
+    dout.fetch(a.dout + (t.first + mine) * a.o_row + head * a.o_head, there, a.head_dim);
+    float delta = 0.f;
+    {
+      Rows<DP> o;
+      o.fetch(a.o + (t.first + mine) * a.o_row + head * a.o_head, there, a.head_dim);
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s)
+      for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) delta = fmaf((float)o.f[s][e], (float)dout.f[s][e], delta);
-    delta += other_half(delta);
-  }
-  const int64_t at = head * a.tokens + t.first + mine;
-  if (there && half == 0) a.delta[at] = delta;
-  const float lse2 = there ? a.lse[at] * LOG2E : 0.f;
-  const int end = a.causal && t.row + S::OWN < t.len ? t.row + S::OWN : t.len;
-  const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;
-  const int last = a.causal && there ? mine : t.len - 1;
-  const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;
-  const float c = a.scale * LOG2E;
-  f32x16 acc[DP / 32];
-#pragma unroll
-  for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
-  sk.put(lds);
-  sv.put(lds + S::TILE);
-  __syncthreads();
-  for (int j0 = 0, turn = 0; j0 < end; j0 += S::WALK, turn ^= 2 * S::TILE) {
-    const bool more = j0 + S::WALK < end;
-    if (more) {
-      sk.fetch(k + (int64_t)(j0 + S::WALK) * a.k_row, a.k_row, t.len - j0 - S::WALK, a.head_dim);
-      sv.fetch(v + (int64_t)(j0 + S::WALK) * a.v_row, a.v_row, t.len - j0 - S::WALK, a.head_dim);
+        for (int e = 0; e < 8; ++e) delta = fmaf((float)o.f[s][e], (float)dout.f[s][e], delta);
+      delta += other_half(delta);
     }
+    const int64_t at = head * a.tokens + t.first + mine;
+    if (there && half == 0) a.delta[at] = delta;
+    const float lse2 = there ? a.lse[at] * LOG2E : 0.f;
+    const int end = a.causal && row + S::OWN < t.len ? row + S::OWN : t.len;
+    const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;
+    const int last = a.causal && there ? mine : t.len - 1;
+    const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;
+    f32x16 acc[DP / 32];
 #pragma unroll
-    for (int sub = 0; sub < S::WALK; sub += 32) {
-      const int j = j0 + sub;
-      if (j >= seen) break;
-      const char* lds_k = lds + turn + sub * Layout<DP>::PITCH;
-      f32x16 s[2];                                                  // scores, and dP
-      products<DP, 2, S::TILE>(s, lds_k, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
-      if (j + 32 > whole) {
-        const int most = last - j - 4 * half;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (walked(r, 0) > most) s[0][r] = -INFINITY;
+    for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
+    sk.put(lds);
+    sv.put(lds + S::TILE);
+    __syncthreads();
+    for (int j0 = 0, turn = 0; j0 < end; j0 += S::WALK, turn ^= 2 * S::TILE) {
+      const bool more = j0 + S::WALK < end;
+      if (more) {
+        sk.fetch(k + (int64_t)(j0 + S::WALK) * a.k_row, a.k_row, t.len - j0 - S::WALK, a.head_dim);
+        sv.fetch(v + (int64_t)(j0 + S::WALK) * a.v_row, a.v_row, t.len - j0 - S::WALK, a.head_dim);
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2)) * (s[1][r] - delta);
-      accumulate<DP, 1, 0>({&acc}, lds_k, {rounded(s[0])});
+      for (int sub = 0; sub < S::WALK; sub += 32) {
+        const int j = j0 + sub;
+        if (j >= seen) break;
+        const char* lds_k = lds + turn + sub * Layout<DP>::PITCH;
+        f32x16 s[2];                                                  // scores, and dP
+        products<DP, 2, S::TILE>(s, lds_k, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
+        if (j + 32 > whole) {
+          int most = last - j - 4 * half;
+          asm volatile("" : "+v"(most));
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (walked(r, 0) > most) s[0][r] = -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2)) * (s[1][r] - delta);
+        accumulate<DP, 1, 0>({&acc}, lds_k, {rounded(s[0])});
+      }
+      if (more) {
+        sk.put(lds + (turn ^ 2 * S::TILE));
+        sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
+      }
+      __syncthreads();
     }
-    if (more) {
-      sk.put(lds + (turn ^ 2 * S::TILE));
-      sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
-    }
-    __syncthreads();
+    store_row<DP>(a.dq + (t.first + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, there);
+    if (tile == t.index) break;
   }
-  store_row<DP>(a.dq + (t.first + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, there);
 }
 
-// dk and dv: 32 keys a wave; the queries of all heads that share the keys are walked, head by head.
-template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_attention_bwd_kv(Args a) {
-  using S = Shape<DP, WAVES>;
-  constexpr int WALK = 32, TILE = S::SUB, BOTH = 2 * TILE + 2 * WALK * (int)sizeof(float);      // queries, do, lse, delta
+// One set of accumulators from the waves of one group to those of the other, which add it to theirs: rows of 16 bytes a lane.
+template <int DP>
+__device__ __forceinline__ void hand_over(char* lds, int wave, const f32x16 (&acc)[DP / 32]) {
+  f32x4* to = reinterpret_cast<f32x4*>(lds) + wave * (DP / 32 * 4) * 64 + (threadIdx.x & 63);
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) to[(m * 4 + g) * 64] = f32x4{acc[m][4 * g], acc[m][4 * g + 1], acc[m][4 * g + 2], acc[m][4 * g + 3]};
+}
+template <int DP>
+__device__ __forceinline__ void take_over(const char* lds, int wave, f32x16 (&acc)[DP / 32]) {
+  const f32x4* from = reinterpret_cast<const f32x4*>(lds) + wave * (DP / 32 * 4) * 64 + (threadIdx.x & 63);
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 v = from[(m * 4 + g) * 64];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[m][4 * g + e] += v[e];
+    }
+}
+
+// dk and dv: 32 keys a wave; the queries of all heads that share the keys are walked, head by head, 32 rows a step for each of GROUPS sets of
+// WAVES waves.  Two sets share the keys (and the sums, which meet at the end) where the key tiles are no more than the compute units: one sequence of
+// 8192, causal, head width 128, 16 heads on 8 of keys: 630 us against 928 with one set; on 16 of keys, two workgroups of one set a unit, 640 against 585.
+template <int DP, int WAVES, int GROUPS>
+__global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_attention_bwd_kv(Args a) {
+  constexpr int OWN = 32 * WAVES, SUB = 32 * Layout<DP>::PITCH;
+  constexpr int WALK = 32 * GROUPS, TILE = GROUPS * SUB, BOTH = 2 * TILE + 2 * WALK * (int)sizeof(float);      // queries, do, lse, delta
   // Wide heads: the accumulators of dk and dv take 2 DP registers a lane, k and v another DP; with v in the LDS two waves fit a SIMD.
   constexpr bool V_IN_LDS = DP > 64;
   __shared__ __attribute__((aligned(16))) char lds[2 * BOTH];
-  __shared__ __attribute__((aligned(16))) char lds_v[V_IN_LDS ? S::OWN * Layout<DP>::PITCH : 16];
+  __shared__ __attribute__((aligned(16))) char lds_v[V_IN_LDS ? OWN * Layout<DP>::PITCH : 16];
+  static_assert(GROUPS == 1 || 2 * BOTH >= WAVES * 64 * DP / 2 * 4);
   const int kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads;
   Tile t;
-  // Causal: the first key tiles have the most queries.  The order is first, second, ..., middle, last, last but one, ...: workgroups half the
-  // grid apart, which share a compute unit where all of them fit the chip at once, have equal work together.
-  const int order = blockIdx.x / a.kv_heads, upper = (a.slots + 1) / 2;
-  if (!find_tile<S::OWN>(a, order < upper ? order : a.slots - 1 - (order - upper), t)) return;
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int first = t.row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
-  const bool there = mine < t.len;
+  if (!find_tile<OWN>(a, blockIdx.x / a.kv_heads, t)) return;
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES;
+  const int set = GROUPS == 1 ? 0 : (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES;
   const float c = a.scale * LOG2E;
-  const int begin = a.causal ? t.row : 0;                          // the first walked query (t.row is a multiple of 32)
-  const int tiles = (t.len - begin + WALK - 1) / WALK;
-  Stage<DP, WALK, S::THREADS> sq, so;
+  Stage<DP, WALK, 64 * WAVES * GROUPS> sq, so;
   sq.init(a.q_row, a.head_dim);
   so.init(a.o_row, a.head_dim);
   float next_lse = 0.f, next_delta = 0.f;
-  int head = kv * group, i = begin;                                // what is fetched next
-  auto fetch = [&] {
-    const int64_t row = t.first + i;
-    sq.fetch(a.q + row * a.q_row + head * a.q_head, a.q_row, t.len - i, a.head_dim);
-    so.fetch(a.dout + row * a.o_row + head * a.o_head, a.o_row, t.len - i, a.head_dim);
-    if (threadIdx.x < WALK) {
-      // rows past the last: exp2(-inf) = 0
-      const bool row_there = i + (int)threadIdx.x < t.len;
-      const int64_t at = head * a.tokens + row + threadIdx.x;
-      next_lse = row_there ? a.lse[at] * LOG2E : INFINITY;
-      next_delta = row_there ? a.delta[at] : 0.f;
-    }
-    i += WALK;
-    if (i >= t.len) { i = begin; ++head; }
-  };
-  auto put = [&](char* to) {
-    sq.put(to);
-    so.put(to + TILE);
-    if (threadIdx.x < WALK) {
-      reinterpret_cast<float*>(to + 2 * TILE)[threadIdx.x] = next_lse;
-      reinterpret_cast<float*>(to + 2 * TILE)[WALK + threadIdx.x] = next_delta;
-    }
-  };
-  fetch();
-  char* const own_v = lds_v + S::SUB * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Rows<DP> k, v;
-  k.fetch(a.k + (t.first + mine) * a.k_row + kv * a.k_head, there, a.head_dim);
-  v.fetch(a.v + (t.first + mine) * a.v_row + kv * a.v_head, there, a.head_dim);
-  if (V_IN_LDS) {
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) *reinterpret_cast<bf16x8*>(own_v + Layout<DP>::at(lane & 31, 2 * s + half)) = v.f[s];
-  }
-  f32x16 dk[DP / 32], dv[DP / 32];
-#pragma unroll
-  for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
-  put(lds);
-  __syncthreads();
-  int at = begin;                                                  // what is used now
-  for (int n = tiles * group, turn = 0; n > 0; --n, turn ^= 1) {
-    char* const now = lds + turn * BOTH;
-    if (n > 1) fetch();
-    if (first < t.len && !(a.causal && at + WALK <= first)) {
-      f32x16 s[2];                                                  // scores, and dP
-      products<DP, 2, TILE>(s, now, [&](int which, int p, int base) {
-        if (!which) return k.f[p];
-        return V_IN_LDS ? *reinterpret_cast<const bf16x8*>(own_v + (base ^ p << 5)) : v.f[p];
-      });
-      if (a.causal && at < first + 31) {
-        const int least = mine - at - 4 * half;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (walked(r, 0) < least) s[0][r] = -INFINITY;
+#pragma nounroll
+  for (int tile = t.index;; tile = t.other) {
+    const int row = tile * OWN, first = row + 32 * wave, mine = first + (lane & 31);
+    const bool there = mine < t.len;
+    const int begin = a.causal ? row : 0;                            // the first walked query
+    int head = kv * group, i = begin, next = begin;                  // what is fetched next, and the rows under way
+    auto fetch = [&] {
+      const int64_t from = t.first + i;
+      sq.fetch(a.q + from * a.q_row + head * a.q_head, a.q_row, t.len - i, a.head_dim);
+      so.fetch(a.dout + from * a.o_row + head * a.o_head, a.o_row, t.len - i, a.head_dim);
+      next = i;
+      if (threadIdx.x < WALK) {
+        const int64_t at = head * a.tokens + t.first + (i + (int)threadIdx.x < t.len ? i + (int)threadIdx.x : t.len - 1);
+        next_lse = a.lse[at];
+        next_delta = a.delta[at];
       }
-      const float* scalars = reinterpret_cast<const float*>(now + 2 * TILE) + 4 * half;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 l = *reinterpret_cast<const f32x4*>(scalars + 8 * g), d = *reinterpret_cast<const f32x4*>(scalars + WALK + 8 * g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * g + e;
-          s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
-          s[1][r] = s[0][r] * (s[1][r] - d[e]);
-        }
+      i += WALK;
+      if (i >= t.len) { i = begin; ++head; }
+    };
+    auto put = [&](char* to) {
+      sq.put(to);
+      so.put(to + TILE);
+      if (threadIdx.x < WALK) {
+        // rows past the last: exp2(-inf) = 0
+        reinterpret_cast<float*>(to + 2 * TILE)[threadIdx.x] = next + (int)threadIdx.x < t.len ? next_lse * LOG2E : INFINITY;
+        reinterpret_cast<float*>(to + 2 * TILE)[WALK + threadIdx.x] = next_delta;
       }
-      accumulate<DP, 2, TILE>({&dk, &dv}, now, {rounded(s[1]), rounded(s[0])});
+    };
+    fetch();
+    char* const own_v = lds_v + SUB * wave;
+    Rows<DP> k, v;
+    k.fetch(a.k + (t.first + mine) * a.k_row + kv * a.k_head, there, a.head_dim);
+    v.fetch(a.v + (t.first + mine) * a.v_row + kv * a.v_head, there, a.head_dim);
+    if (V_IN_LDS && set == 0) {
+#pragma unroll
+      for (int s = 0; s < DP / 16; ++s) *reinterpret_cast<bf16x8*>(own_v + Layout<DP>::at(lane & 31, 2 * s + half)) = v.f[s];
     }
-    at += WALK;
-    if (at >= t.len) at = begin;
-    if (n > 1) put(lds + (turn ^ 1) * BOTH);
+    f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
+    put(lds);
     __syncthreads();
+    int at = begin;                                                  // what is used now
+    for (int n = (t.len - begin + WALK - 1) / WALK * group, turn = 0; n > 0; --n, turn ^= 1) {
+      const char* const now = lds + turn * BOTH;
+      if (n > 1) fetch();
+      const int from = at + 32 * set;
+      if (first < t.len && from < t.len && !(a.causal && from + 32 <= first)) {
+        f32x16 s[2];                                                  // scores, and dP
+        products<DP, 2, TILE>(s, now + set * SUB, [&](int which, int p, int base) {
+          if (!which) return k.f[p];
+          return V_IN_LDS ? *reinterpret_cast<const bf16x8*>(own_v + (base ^ p << 5)) : v.f[p];
+        });
+        if (a.causal && from < first + 31) {
+          int least = mine - from - 4 * half;
+          asm volatile("" : "+v"(least));
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (walked(r, 0) < least) s[0][r] = -INFINITY;
+        }
+        const float* scalars = reinterpret_cast<const float*>(now + 2 * TILE) + 32 * set + 4 * half;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 l = *reinterpret_cast<const f32x4*>(scalars + 8 * g), d = *reinterpret_cast<const f32x4*>(scalars + WALK + 8 * g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * g + e;
+            s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
+            s[1][r] = s[0][r] * (s[1][r] - d[e]);
+          }
+        }
+        accumulate<DP, 2, TILE>({&dk, &dv}, now + set * SUB, {rounded(s[1]), rounded(s[0])});
+      }
+      at += WALK;
+      if (at >= t.len) at = begin;
+      if (n > 1) put(lds + (turn ^ 1) * BOTH);
+      __syncthreads();
+    }
+    if (GROUPS == 2) {
+      if (set) hand_over<DP>(lds, wave, dk);
+      __syncthreads();
+      if (!set) take_over<DP>(lds, wave, dk);
+      __syncthreads();
+      if (!set) hand_over<DP>(lds, wave, dv);
+      __syncthreads();
+      if (set) take_over<DP>(lds, wave, dv);
+      __syncthreads();
+    }
+    if (!set) store_row<DP>(a.dk + (t.first + mine) * a.k_row + kv * a.k_head, dk, a.scale, a.head_dim, there);
+    if (GROUPS == 1 || set) store_row<DP>(a.dv + (t.first + mine) * a.v_row + kv * a.v_head, dv, 1.f, a.head_dim, there);
+    if (tile == t.other) break;
   }
-  store_row<DP>(a.dk + (t.first + mine) * a.k_row + kv * a.k_head, dk, a.scale, a.head_dim, there);
-  store_row<DP>(a.dv + (t.first + mine) * a.v_row + kv * a.v_head, dv, 1.f, a.head_dim, there);
 }
 
 int check(const disco_attention_shape* s) {
@@ -545,6 +598,8 @@ Args args_of(const disco_attention_shape& s, const int32_t* starts) {
   return a;
 }
 
+constexpr int COMPUTE_UNITS = 256;
+
 int waves_of(const disco_attention_shape& s) { return s.tokens <= (int64_t)96 * s.sequences ? 1 : 4; }
 
 template <int DP, int WAVES>
@@ -558,7 +613,10 @@ bool backward(Args a, hipStream_t st) {
   a.slots = (int)(a.tokens / (32 * WAVES)) + a.sequences;
   k_attention_bwd_q<DP, WAVES><<<(unsigned)(a.slots * a.heads), 64 * WAVES, 0, st>>>(a);
   if (hipGetLastError() != hipSuccess) return false;
-  k_attention_bwd_kv<DP, WAVES><<<(unsigned)(a.slots * a.kv_heads), 64 * WAVES, 0, st>>>(a);
+  const unsigned grid = (unsigned)(a.slots * a.kv_heads);
+  const int64_t work = a.tokens / (32 * WAVES) * a.kv_heads / (a.causal ? 2 : 1);      // workgroups that have some, nearly
+  if (WAVES == 1 || work > COMPUTE_UNITS) k_attention_bwd_kv<DP, WAVES, 1><<<grid, 64 * WAVES, 0, st>>>(a);
+  else k_attention_bwd_kv<DP, WAVES, WAVES == 1 ? 1 : 2><<<grid, 128 * WAVES, 0, st>>>(a);
   return hipGetLastError() == hipSuccess;
 }
 
