@@ -4,7 +4,9 @@
 //   t = dy + N_pre'(dn),  dx = x_scale t,  du = h_scale gate t,  dh = N_post'(du),  dgate = h_scale t u
 //   N'(g) = rstd (a - [mean a] - zhat mean(a zhat)),  a = g w,  zhat = (z - mean) rstd;  dw = sum over rows g zhat,  db = sum over rows g
 //
-// Bound by memory: a row is read once, kept in registers (8 columns a lane, LANES lanes a row, so that rows of a few hundred columns
+// Bound by memory, and within a tenth of it but for the widest shares of idle lanes (forward 39424 x 512 bf16, a norm before: 32 us, 5.0 TB/s; 10007 x 1001
+// fp32, both norms, an element gate: 42 us, 4.8 TB/s; backward 16384 x 4096, fp32 stream, bf16 branch, both norms: 271 us, 4.5 TB/s; 50432 x 768
+// bf16, where a quarter of the lanes have no columns: 133 us, 3.5 TB/s).  A row is read once, kept in registers (8 columns a lane, LANES lanes a row, so that rows of a few hundred columns
 // share a wave and the widest take 16) and written once.  The variance is summed over the deviations from the mean, which are at
 // hand, not taken as a difference of sums.  The backward pass adds the sums over rows up in registers, one workgroup's rows in the LDS, and
 // the workgroups' in a second kernel, in a fixed order.  Everything is fp32 but what is stored.
@@ -62,7 +64,10 @@ __device__ __forceinline__ Raw load_raw(const void* p, int64_t row, int d, int c
   }
   return r;
 }
+// In a kernel all of whose rows are bf16 the second half is never there and takes no registers.
+template <bool NARROW>
 __device__ __forceinline__ void values(const Raw& r, bool bf16, float (&v)[COLS]) {
+  if (NARROW) bf16 = true;
   if (bf16) {
 #pragma unroll
     for (int e = 0; e < COLS; ++e) v[e] = __uint_as_float(e % 2 ? r.a[e / 2] & 0xffff0000u : r.a[e / 2] << 16);
@@ -170,8 +175,13 @@ __device__ __forceinline__ void statistics(RowSum<LANES>& total, const float (&z
   rstd = 1.f / sqrtf(var * inv_d + eps);
 }
 
-template <int LANES, bool POST, bool PRE>
-__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_block_norm_fwd(Args a) {
+// Waves a SIMD that the kernels' registers are kept to, which the grids go by.
+template <bool POST, bool PRE>
+constexpr int waves_fwd() { return POST && PRE ? 4 : POST || PRE ? 5 : 7; }
+
+template <int LANES, bool POST, bool PRE, bool NARROW>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256, (waves_fwd<POST, PRE>())) void k_block_norm_fwd(Args a) {
+  if (NARROW) a.x_bf16 = a.h_bf16 = 1;
   using R = RowSum<LANES>;
   constexpr int ROWS = R::BLOCK / LANES;
   __shared__ float lds[2][R::BLOCK / 64][2];
@@ -190,15 +200,15 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_block_norm_fwd(Ar
     if (a.x) rx = load_raw(a.x, row, d, col, a.x_bf16);
     if (a.gate == DISCO_GATE_ELEMENT) rg = load_raw(a.gate_values, row, d, col, a.h_bf16);
     float h[COLS], y[COLS];
-    values(rh, a.h_bf16, h);
+    values<NARROW>(rh, a.h_bf16, h);
     float m2 = 0.f, r2 = 0.f, m1 = 0.f, r1 = 0.f;
     if (POST) {
       statistics(total, h, a.post == DISCO_NORM_LAYER, d, col, a.inv_d, a.eps_post, m2, r2);
 #pragma unroll
       for (int e = 0; e < COLS; ++e) h[e] = fmaf((h[e] - m2) * r2, w2[e], b2[e]);
     }
-    if (a.gate == DISCO_GATE_ELEMENT) values(rg, a.h_bf16, g);
-    values(rx, a.x_bf16, y);
+    if (a.gate == DISCO_GATE_ELEMENT) values<NARROW>(rg, a.h_bf16, g);
+    values<NARROW>(rx, a.x_bf16, y);
 #pragma unroll
     for (int e = 0; e < COLS; ++e) y[e] = fmaf(a.x_scale, y[e], a.h_scale * g[e] * h[e]);
     if (there) store(a.out_y, row, d, col, a.x_bf16, y);
@@ -212,8 +222,14 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_block_norm_fwd(Ar
   }
 }
 
-template <int LANES, bool POST, bool PRE>
-__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_block_norm_bwd(Args a) {
+// Waves a SIMD that the backward kernel's registers are kept to: what hides its loads is other rows' waves (50432 x 768 bf16, a norm before the next
+// block, a gate for each channel: 204 us with 3 waves, 140 with 4; asking for the next row's data a row ahead costs the registers of a wave and 180).
+template <bool POST, bool PRE, bool NARROW>
+constexpr int waves_bwd() { return POST && PRE ? (NARROW ? 3 : 2) : NARROW ? 4 : 3; }
+
+template <int LANES, bool POST, bool PRE, bool NARROW>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256, (waves_bwd<POST, PRE, NARROW>())) void k_block_norm_bwd(Args a) {
+  if (NARROW) a.x_bf16 = a.h_bf16 = 1;
   using R = RowSum<LANES>;
   constexpr int ROWS = R::BLOCK / LANES;
   __shared__ float lds[2][R::BLOCK / 64][2];
@@ -241,11 +257,11 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_block_norm_bwd(Ar
     if (a.gate == DISCO_GATE_ELEMENT) rg = load_raw(a.gate_values, row, d, col, a.h_bf16);
     const float* st = a.stats + row * 4;
     float t[COLS];
-    values(rt, a.x_bf16, t);
+    values<NARROW>(rt, a.x_bf16, t);
     if (PRE) {
       float y[COLS], dn[COLS], p[COLS], q[COLS];
-      values(ry, a.x_bf16, y);
-      values(rn, a.h_bf16, dn);
+      values<NARROW>(ry, a.x_bf16, y);
+      values<NARROW>(rn, a.h_bf16, dn);
       const float m1 = st[2], r1 = st[3];
 #pragma unroll
       for (int e = 0; e < COLS; ++e) {
@@ -269,8 +285,8 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_block_norm_bwd(Ar
       if (there && a.dx) store(a.dx, row, d, col, a.x_bf16, dx);
     }
     float h[COLS];
-    values(rh, a.h_bf16, h);
-    if (a.gate == DISCO_GATE_ELEMENT) values(rg, a.h_bf16, g);
+    values<NARROW>(rh, a.h_bf16, h);
+    if (a.gate == DISCO_GATE_ELEMENT) values<NARROW>(rg, a.h_bf16, g);
     float m2 = 0.f, r2 = 1.f;
     if (POST) { m2 = st[0]; r2 = st[1]; }
     float du[COLS], dg[COLS];
@@ -328,6 +344,7 @@ __global__ __launch_bounds__(1024) void k_block_norm_sums(Args a, int blocks) {
   float s = 0.f;
   if (c < a.d) {
     const float* p = a.parts + (int64_t)blockIdx.y * a.d + c;
+#pragma unroll 16
     for (int b = share; b < blocks; b += 16) s += p[(int64_t)b * a.wanted * a.d];
   }
   part[share][threadIdx.x & 63] = s;
@@ -369,14 +386,19 @@ int lanes_of(int64_t d) {
   while (lanes * COLS < d) lanes *= 2;
   return lanes;
 }
-// Workgroups: each walks its rows with its parameters at hand
-int64_t blocks_of(int64_t rows, int64_t d, int64_t most) {
-  const int lanes = lanes_of(d);
-  const int64_t each = lanes > 256 ? 1 : 256 / lanes, all = (rows + each - 1) / each;
+bool narrow_of(const disco_block_norm_shape& s) { return s.x_dtype == DISCO_BF16 && s.h_dtype == DISCO_BF16; }
+// Workgroups: what the chip holds at once.  Each walks its rows with its parameters at hand, and none waits for another to end (39424 x 512 bf16 forward,
+// 5 waves a SIMD: 32 us; 3.2 times as many workgroups 41, one for each four rows 79).
+int64_t blocks_of(const disco_block_norm_shape& s, int waves) {
+  const int lanes = lanes_of(s.d), each = lanes > 256 ? lanes / 256 : 1;
+  const int64_t rows = lanes > 256 ? 1 : 256 / lanes, all = (s.rows + rows - 1) / rows, most = 256 * (waves < each ? 1 : waves / each);
   return all < most ? all : most;
 }
-constexpr int64_t FWD_BLOCKS = 4096, BWD_BLOCKS = 1024;
-
+template <class F>
+void with_bool(bool v, F f) {
+  if (v) f(std::true_type());
+  else f(std::false_type());
+}
 template <class F>
 void with_lanes(int64_t d, F f) {
   switch (lanes_of(d)) {
@@ -390,6 +412,19 @@ void with_lanes(int64_t d, F f) {
   }
 }
 
+// f(a norm after the block, one before the next, all rows bf16), as constants
+template <class F>
+void with_form(const disco_block_norm_shape& s, F f) {
+  with_bool(s.post != DISCO_NORM_NONE, [&](auto post) {
+    with_bool(s.pre != DISCO_NORM_NONE, [&](auto pre) { with_bool(narrow_of(s), [&](auto narrow) { f(post, pre, narrow); }); });
+  });
+}
+int64_t bwd_blocks(const disco_block_norm_shape& s) {
+  int64_t n = 0;
+  with_form(s, [&](auto post, auto pre, auto narrow) { n = blocks_of(s, waves_bwd<post(), pre(), narrow()>()); });
+  return n;
+}
+
 }  // namespace
 }  // namespace disco
 
@@ -397,7 +432,7 @@ using namespace disco;
 
 extern "C" size_t disco_block_norm_workspace_bytes(const disco_block_norm_shape* shape) {
   if (check(shape) != DISCO_OK) return 0;
-  return align_up((size_t)blocks_of(shape->rows, shape->d, BWD_BLOCKS) * SUMS * (size_t)shape->d * sizeof(float));
+  return align_up((size_t)bwd_blocks(*shape) * SUMS * (size_t)shape->d * sizeof(float));
 }
 
 extern "C" int disco_block_norm_fwd(const disco_block_norm_shape* shape, const void* x, const void* h, const void* gate, const float* w_post,
@@ -416,14 +451,13 @@ extern "C" int disco_block_norm_fwd(const disco_block_norm_shape* shape, const v
     if (!aligned(p, 0)) return DISCO_ERR_UNSUPPORTED;
   a.x = x; a.h = h; a.gate_values = gate; a.w_post = w_post; a.b_post = b_post; a.w_pre = w_pre; a.b_pre = b_pre;
   a.out_y = y; a.out_n = n; a.stats = stats;
-  const unsigned grid = (unsigned)blocks_of(a.rows, a.d, FWD_BLOCKS);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   with_lanes(a.d, [&](auto lanes) {
     constexpr int L = lanes(), B = L > 256 ? L : 256;
-    if (a.post && a.pre) k_block_norm_fwd<L, true, true><<<grid, B, 0, st>>>(a);
-    else if (a.post) k_block_norm_fwd<L, true, false><<<grid, B, 0, st>>>(a);
-    else if (a.pre) k_block_norm_fwd<L, false, true><<<grid, B, 0, st>>>(a);
-    else k_block_norm_fwd<L, false, false><<<grid, B, 0, st>>>(a);
+    with_form(*shape, [&](auto post, auto pre, auto narrow) {
+      const unsigned grid = (unsigned)blocks_of(*shape, waves_fwd<post(), pre()>());
+      k_block_norm_fwd<L, post(), pre(), narrow()><<<grid, B, 0, st>>>(a);
+    });
   });
   return hipGetLastError() == hipSuccess ? DISCO_OK : DISCO_ERR_HIP;
 }
@@ -456,14 +490,11 @@ extern "C" int disco_block_norm_bwd(const disco_block_norm_shape* shape, const v
   if (a.pre) { a.sums[3] = dw_pre; a.sums[4] = db_pre; }
   for (float* s : a.sums) a.wanted += s != nullptr;
   a.parts = static_cast<float*>(workspace);
-  const unsigned grid = (unsigned)blocks_of(a.rows, a.d, BWD_BLOCKS);
+  const unsigned grid = (unsigned)bwd_blocks(*shape);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   with_lanes(a.d, [&](auto lanes) {
     constexpr int L = lanes(), B = L > 256 ? L : 256;
-    if (a.post && a.pre) k_block_norm_bwd<L, true, true><<<grid, B, 0, st>>>(a);
-    else if (a.post) k_block_norm_bwd<L, true, false><<<grid, B, 0, st>>>(a);
-    else if (a.pre) k_block_norm_bwd<L, false, true><<<grid, B, 0, st>>>(a);
-    else k_block_norm_bwd<L, false, false><<<grid, B, 0, st>>>(a);
+    with_form(*shape, [&](auto post, auto pre, auto narrow) { k_block_norm_bwd<L, post(), pre(), narrow()><<<grid, B, 0, st>>>(a); });
   });
   if (hipGetLastError() != hipSuccess) return DISCO_ERR_HIP;
   if (a.wanted && grid > 1) k_block_norm_sums<<<dim3((unsigned)((a.d + 63) / 64), (unsigned)a.wanted), 1024, 0, st>>>(a, (int)grid);
