@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 
 # torch owns the device memory and the streams that are handed to the library, so its HIP runtime
 # must be the one in the process: load it before libdisco.so, which then binds to the same
@@ -295,18 +296,17 @@ def disco_block_norm_bwd(shape, dy, dn, h, y, gate, w_post, b_post, w_pre, stats
 _DTYPES = {torch.float32: DISCO_F32, torch.bfloat16: DISCO_BF16}
 
 
-def _addresses(tensors):
-    return (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
-
-
 def _listed(tensors):
     """Host arrays of a list of dense torch tensors: addresses, numbers of elements, types (-1, which the library refuses, where it has none)."""
-    n = len(tensors)
-    for t in tensors:
-        if not t.is_contiguous():
-            raise ValueError("gradients have to be contiguous")
-    return (_addresses(tensors), (ctypes.c_int64 * n)(*[t.numel() for t in tensors]),
-            (ctypes.c_int32 * n)(*[_DTYPES.get(t.dtype, -1) for t in tensors]))
+    t = torch.Tensor
+    if not all(map(t.is_contiguous, tensors)):
+        raise ValueError("gradients have to be contiguous")
+    return (array("q", map(t.data_ptr, tensors)), array("q", map(t.numel, tensors)),
+            array("i", [_DTYPES.get(d, -1) for d in map(t.dtype.__get__, tensors)]))
+
+
+def _at(a):
+    return a.buffer_info()[0]
 
 
 def disco_grad_workspace_bytes(count: int) -> int:
@@ -316,7 +316,7 @@ def disco_grad_workspace_bytes(count: int) -> int:
 def disco_grad_norm(src, norm, workspace, workspace_bytes, accumulate=0, stream=None, check=True) -> int:
     """`src`: a list of torch tensors, contiguous, fp32 or bf16."""
     at, elements, dtypes = _listed(src)
-    st = _lib.disco_grad_norm(at, elements, dtypes, len(src), int(accumulate), _ptr(norm), _ptr(workspace), workspace_bytes, _stream_ptr(stream))
+    st = _lib.disco_grad_norm(_at(at), _at(elements), _at(dtypes), len(src), int(accumulate), _ptr(norm), _ptr(workspace), workspace_bytes, _stream_ptr(stream))
     if check and st != DISCO_OK:
         raise DiscoError(st, "disco_grad_norm")
     return st
@@ -328,9 +328,9 @@ def disco_grad_clip(src, dst, max_norm, given, norm, workspace, workspace_bytes,
     to = at
     if dst is not src:
         to, n, types = _listed(dst)
-        if list(n) != list(elements) or list(types) != list(dtypes):
+        if n != elements or types != dtypes:
             raise ValueError("dst has other sizes or types than src")
-    st = _lib.disco_grad_clip(at, to, elements, dtypes, len(src), max_norm, _ptr(given), _ptr(norm), _ptr(workspace), workspace_bytes,
+    st = _lib.disco_grad_clip(_at(at), _at(to), _at(elements), _at(dtypes), len(src), max_norm, _ptr(given), _ptr(norm), _ptr(workspace), workspace_bytes,
                               _stream_ptr(stream))
     if check and st != DISCO_OK:
         raise DiscoError(st, "disco_grad_clip")

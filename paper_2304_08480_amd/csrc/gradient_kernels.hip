@@ -127,23 +127,37 @@ __global__ __launch_bounds__(THREADS) void k_grad_squares(Table table, double* p
   if (threadIdx.x == 0) parts[blockIdx.x] = s;
 }
 
-__global__ __launch_bounds__(1024) void k_grad_norm(const double* parts, int n, int accumulate, float* norm) {
+__device__ __forceinline__ double sum_of(const double* parts, int n) {
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += 1024) s += parts[i];
-  s = block_sum(s);
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += blockDim.x) s += parts[i];
+  return block_sum(s);
+}
+
+__global__ __launch_bounds__(1024) void k_grad_norm(const double* parts, int n, int accumulate, float* norm) {
+  double s = sum_of(parts, n);
   if (threadIdx.x == 0) {
     if (accumulate) s = fma((double)*norm, (double)*norm, s);
     *norm = (float)sqrt(s);
   }
 }
 
-__global__ __launch_bounds__(THREADS) void k_grad_scale(Table table, float max_norm, const float* norm) {
-  const float taken = *norm;
+// The pieces run from the end of a tensor (and the host's tables from the end of the list): what the norm read last is still in the last-level
+// cache.  Few partial sums (n > 0) are joined by every workgroup for itself, the norm's own launch is saved: all of them take the same order, so
+// they come to the same norm, and the first one stores it.
+__global__ __launch_bounds__(THREADS) void k_grad_scale(Table table, float max_norm, float* norm, const double* parts, int n) {
+  float taken;
+  if (n) {
+    taken = (float)sqrt(sum_of(parts, n));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = taken;
+  } else {
+    taken = *norm;
+  }
   const float quotient = max_norm / (taken + 1e-6f), factor = quotient < 1.f ? quotient : taken == taken ? 1.f : taken;
   for (int p = blockIdx.x; p < table.pieces; p += gridDim.x) {
     const Tensor& t = table.t[tensor_of(table, p)];
     if (factor == 1.f && t.src == t.dst) continue;
-    const int64_t from = (int64_t)(p - t.first) * PIECE + threadIdx.x * 8;
+    const int64_t from = ((t.n + PIECE - 1) / PIECE - 1 - (p - t.first)) * PIECE + threadIdx.x * 8;
     Eight r[UNROLL];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) r[u] = load8(t.src, from + u * THREADS * 8, t.n, t.bf16);
@@ -181,17 +195,18 @@ int check(const void* const* src, void* const* dst, const int64_t* elements, con
   return all <= 0x7fffffff ? DISCO_OK : DISCO_ERR_SHAPE;       // pieces are counted in 32 bits
 }
 
-// f(table) for every TABLE tensors that have elements
+// f(table) for every TABLE tensors that have elements, from the list's first or from its last
 template <class F>
-bool tables(const void* const* src, void* const* dst, const int64_t* elements, const int32_t* dtypes, int64_t count, F f) {
+bool tables(const void* const* src, void* const* dst, const int64_t* elements, const int32_t* dtypes, int64_t count, bool backwards, F f) {
   Table table;
   table.count = table.pieces = 0;
-  for (int64_t i = 0; i < count; ++i) {
+  for (int64_t k = 0; k < count; ++k) {
+    const int64_t i = backwards ? count - 1 - k : k;
     if (elements[i]) {
       table.t[table.count++] = Tensor{src[i], dst ? dst[i] : nullptr, elements[i], table.pieces, dtypes[i] == DISCO_BF16};
       table.pieces += (int32_t)((elements[i] + PIECE - 1) / PIECE);
     }
-    if (table.count == TABLE || (i + 1 == count && table.count)) {
+    if (table.count == TABLE || (k + 1 == count && table.count)) {
       if (!f(table)) return false;
       table.count = table.pieces = 0;
     }
@@ -200,17 +215,22 @@ bool tables(const void* const* src, void* const* dst, const int64_t* elements, c
 }
 unsigned grid_of(const Table& t) { return (unsigned)(t.pieces < BLOCKS ? t.pieces : BLOCKS); }
 
-bool norm_of(const void* const* src, const int64_t* elements, const int32_t* dtypes, int64_t count, int accumulate, float* norm, double* parts, hipStream_t st) {
+// The squares' partial sums: how many (-1: a launch failed)
+int squares(const void* const* src, const int64_t* elements, const int32_t* dtypes, int64_t count, double* parts, hipStream_t st) {
   int n = 0;
-  const bool ok = tables(src, nullptr, elements, dtypes, count, [&](const Table& table) {
+  const bool ok = tables(src, nullptr, elements, dtypes, count, false, [&](const Table& table) {
     k_grad_squares<<<grid_of(table), THREADS, 0, st>>>(table, parts + n);
     n += (int)grid_of(table);
     return hipGetLastError() == hipSuccess;
   });
-  if (!ok) return false;
+  return ok ? n : -1;
+}
+bool norm_of(const double* parts, int n, int accumulate, float* norm, hipStream_t st) {
   k_grad_norm<<<1, 1024, 0, st>>>(parts, n, accumulate, norm);
   return hipGetLastError() == hipSuccess;
 }
+// Partial sums that every workgroup joins for itself: up to four a thread.
+constexpr int FEW = 4 * THREADS;
 
 bool workspace_ok(const void* ws, size_t bytes, int64_t count) {
   return ws && (reinterpret_cast<uintptr_t>(ws) & 255) == 0 && bytes >= disco_grad_workspace_bytes(count);
@@ -231,8 +251,10 @@ extern "C" int disco_grad_norm(const void* const* src, const int64_t* elements, 
   if (const int st = check(src, nullptr, elements, dtypes, count, false)) return st;
   if (reinterpret_cast<uintptr_t>(norm) & 3) return DISCO_ERR_UNSUPPORTED;
   if (!workspace_ok(workspace, workspace_bytes, count)) return DISCO_ERR_WORKSPACE;
-  return norm_of(src, elements, dtypes, count, accumulate, norm, static_cast<double*>(workspace), static_cast<hipStream_t>(hip_stream)) ? DISCO_OK
-                                                                                                                                     : DISCO_ERR_HIP;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  double* parts = static_cast<double*>(workspace);
+  const int n = squares(src, elements, dtypes, count, parts, st);
+  return n >= 0 && norm_of(parts, n, accumulate, norm, st) ? DISCO_OK : DISCO_ERR_HIP;
 }
 
 extern "C" int disco_grad_clip(const void* const* src, void* const* dst, const int64_t* elements, const int32_t* dtypes, int64_t count, float max_norm,
@@ -243,13 +265,21 @@ extern "C" int disco_grad_clip(const void* const* src, void* const* dst, const i
   if ((reinterpret_cast<uintptr_t>(norm) | reinterpret_cast<uintptr_t>(given)) & 3) return DISCO_ERR_UNSUPPORTED;
   if (!workspace_ok(workspace, workspace_bytes, count)) return DISCO_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (!given && !norm_of(src, elements, dtypes, count, 0, norm, static_cast<double*>(workspace), st)) return DISCO_ERR_HIP;
-  if (given && given != norm) {
+  double* parts = static_cast<double*>(workspace);
+  int n = 0;
+  if (!given) {
+    n = squares(src, elements, dtypes, count, parts, st);
+    if (n < 0) return DISCO_ERR_HIP;
+    if (n == 0 || n > FEW) {
+      if (!norm_of(parts, n, 0, norm, st)) return DISCO_ERR_HIP;
+      n = 0;
+    }
+  } else if (given != norm) {
     k_grad_keep<<<1, 64, 0, st>>>(given, norm);
     if (hipGetLastError() != hipSuccess) return DISCO_ERR_HIP;
   }
-  return tables(src, dst, elements, dtypes, count, [&](const Table& table) {
-           k_grad_scale<<<grid_of(table), THREADS, 0, st>>>(table, max_norm, norm);
+  return tables(src, dst, elements, dtypes, count, true, [&](const Table& table) {
+           k_grad_scale<<<grid_of(table), THREADS, 0, st>>>(table, max_norm, norm, parts, n);
            return hipGetLastError() == hipSuccess;
          }) ? DISCO_OK : DISCO_ERR_HIP;
 }
