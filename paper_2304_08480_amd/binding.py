@@ -128,9 +128,7 @@ _lib = _load()
 
 
 def _ptr(x):
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
     return x.data_ptr()       # torch tensor
 
@@ -296,13 +294,16 @@ def disco_block_norm_bwd(shape, dy, dn, h, y, gate, w_post, b_post, w_pre, stats
 _DTYPES = {torch.float32: DISCO_F32, torch.bfloat16: DISCO_BF16}
 
 
-def _listed(tensors):
-    """Host arrays of a list of dense torch tensors: addresses, numbers of elements, types (-1, which the library refuses, where it has none)."""
+def _dense(tensors):
+    """Host array of the addresses of dense torch tensors, their numbers of elements and types."""
     t = torch.Tensor
     if not all(map(t.is_contiguous, tensors)):
         raise ValueError("gradients have to be contiguous")
-    return (array("q", map(t.data_ptr, tensors)), array("q", map(t.numel, tensors)),
-            array("i", [_DTYPES.get(d, -1) for d in map(t.dtype.__get__, tensors)]))
+    return array("q", map(t.data_ptr, tensors)), list(map(t.numel, tensors)), list(map(t.dtype.__get__, tensors))
+
+
+def _codes(types):
+    return array("i", [_DTYPES.get(t, -1) for t in types])      # -1: refused by the library
 
 
 def _at(a):
@@ -315,8 +316,10 @@ def disco_grad_workspace_bytes(count: int) -> int:
 
 def disco_grad_norm(src, norm, workspace, workspace_bytes, accumulate=0, stream=None, check=True) -> int:
     """`src`: a list of torch tensors, contiguous, fp32 or bf16."""
-    at, elements, dtypes = _listed(src)
-    st = _lib.disco_grad_norm(_at(at), _at(elements), _at(dtypes), len(src), int(accumulate), _ptr(norm), _ptr(workspace), workspace_bytes, _stream_ptr(stream))
+    at, sizes, types = _dense(src)
+    elements, dtypes = array("q", sizes), _codes(types)
+    st = _lib.disco_grad_norm(_at(at), _at(elements), _at(dtypes), len(src), int(accumulate), _ptr(norm), _ptr(workspace), workspace_bytes,
+                              _stream_ptr(stream))
     if check and st != DISCO_OK:
         raise DiscoError(st, "disco_grad_norm")
     return st
@@ -324,14 +327,15 @@ def disco_grad_norm(src, norm, workspace, workspace_bytes, accumulate=0, stream=
 
 def disco_grad_clip(src, dst, max_norm, given, norm, workspace, workspace_bytes, stream=None, check=True) -> int:
     """`src`, `dst`: lists of torch tensors, contiguous, fp32 or bf16, of the same sizes and types; `dst` may be `src`."""
-    at, elements, dtypes = _listed(src)
+    at, sizes, types = _dense(src)
     to = at
     if dst is not src:
-        to, n, types = _listed(dst)
-        if n != elements or types != dtypes:
+        to, *rest = _dense(dst)
+        if rest != [sizes, types]:
             raise ValueError("dst has other sizes or types than src")
-    st = _lib.disco_grad_clip(_at(at), _at(to), _at(elements), _at(dtypes), len(src), max_norm, _ptr(given), _ptr(norm), _ptr(workspace), workspace_bytes,
-                              _stream_ptr(stream))
+    elements, dtypes = array("q", sizes), _codes(types)
+    st = _lib.disco_grad_clip(_at(at), _at(to), _at(elements), _at(dtypes), len(src), max_norm, _ptr(given), _ptr(norm), _ptr(workspace),
+                              workspace_bytes, _stream_ptr(stream))
     if check and st != DISCO_OK:
         raise DiscoError(st, "disco_grad_clip")
     return st

@@ -44,36 +44,64 @@ struct Args {
   int32_t slots;
 };
 
-// Which tile of T rows of which sequence a workgroup has.  Sequence s owns the slots from starts[s] / T + s on: at least as many as it has
-// tiles, whatever its start, so the tiles are found with no table and no count of them, for at most `sequences` idle workgroups more.  The
-// search is 64 ways wide: two rounds of loads for thousands of sequences.  What it reads is kept within [0, tokens].
+// Which tile of T rows of which sequence a workgroup has.  Causal: tile i of queries has i + 1 tiles of keys to walk, the i-th last tile of keys
+// i + 1 of queries.
 //
-// Causal: the later a tile of queries (the earlier a tile of keys), the more it has to do.  A workgroup takes a tile and the one that lies as far
-// from the sequence's other end, so that all of a sequence's workgroups have the same work.
-struct Tile { int64_t first; int32_t len, index, other; };        // the sequence's first row and length; index <= other, equal: one tile
-template <int T>
+// Up to 64 sequences: the tiles with the most to do first, so that the workgroups that take longest are not the last to start.  A lane has a
+// sequence; N(k), the number of tiles that are the k-th or a later one of their sequence (that have at least k to do), falls with k, and slot n's tile has the
+// largest k with N(k) > n.  (24 documents of 1 to 2048 tokens, 16 heads of 128, forward: PAIRED us, LONGEST.)
+//
+// More: sequence s owns the slots from starts[s] / T + s on, at least as many as it has tiles, whatever its start, so the tiles are found with no table
+// and no count of them, for at most `sequences` idle workgroups more.  The search is 64 ways wide: two rounds of loads for thousands of sequences.
+//
+// What is read from `starts` is kept within [0, tokens].
+struct Tile { int64_t first; int32_t len, row; };        // the sequence's first row and length, the tile's first row in it
+template <int T, bool KEYS>
 __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
   const int lane = threadIdx.x & 63, tokens = (int)a.tokens;
   auto start = [&](int s) { const int v = a.starts[s]; return v < 0 ? 0 : v > tokens ? tokens : v; };
-  int lo = 0, n = a.sequences;
-  for (;;) {
-    const int step = (n + 63) / 64, s = lo + lane * step;
-    const bool below = lane * step < n && start(s) / T + s <= slot;
-    const int count = __popcll(__ballot(below));
-    if (count == 0) return false;
-    const int taken = (count - 1) * step;
-    lo += taken;
-    n = n - taken < step ? n - taken : step;
-    if (step == 1) break;
+  int from, len, index;
+  if (a.sequences <= 64) {
+    const bool there = lane < a.sequences;
+    const int first = there ? start(lane) : 0, mine = there ? start(lane + 1) - first : 0, tiles = mine > 0 ? (mine - 1) / T + 1 : 0;
+    auto later = [&](int k) { return wave_reduce(tiles >= k ? tiles - k + 1 : 0, [](int x, int y) { return x + y; }); };
+    if (slot >= later(1)) return false;
+    int k = 1, over = wave_reduce(tiles, [](int x, int y) { return x > y ? x : y; }) + 1, before = 0;      // N(k) > slot >= N(over) = before
+    while (over - k > 1) {
+      const int mid = (k + over) / 2, n = later(mid);
+      if (n > slot) k = mid;
+      else { over = mid; before = n; }
+    }
+    const uint64_t members = __ballot(tiles >= k);
+    const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(members >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)members, 0));
+    const uint64_t owner = __ballot(tiles >= k && rank == slot - before);
+    if (owner == 0) return false;
+    const int s = __ffsll((unsigned long long)owner) - 1;
+    from = __builtin_amdgcn_readlane(first, s);
+    len = __builtin_amdgcn_readlane(mine, s);
+    index = k - 1;
+  } else {
+    int lo = 0, n = a.sequences;
+    for (;;) {
+      const int step = (n + 63) / 64, s = lo + lane * step;
+      const bool below = lane * step < n && start(s) / T + s <= slot;
+      const int count = __popcll(__ballot(below));
+      if (count == 0) return false;
+      const int taken = (count - 1) * step;
+      lo += taken;
+      n = n - taken < step ? n - taken : step;
+      if (step == 1) break;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    from = __builtin_amdgcn_readfirstlane(start(lo));
+    len = __builtin_amdgcn_readfirstlane(start(lo + 1)) - from;
+    index = slot - (from / T + lo);
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  const int from = start(lo), to = start(lo + 1);
-  t.first = __builtin_amdgcn_readfirstlane(from);
-  t.len = __builtin_amdgcn_readfirstlane(to - from);
-  t.index = __builtin_amdgcn_readfirstlane(slot - (from / T + lo));
-  const int count = (t.len + T - 1) / T;
-  t.other = a.causal ? count - 1 - t.index : t.index;
-  return t.index < count && t.index <= t.other;
+  const int count = (len + T - 1) / T;
+  t.first = from;
+  t.len = len;
+  t.row = (KEYS && a.causal ? count - 1 - index : index) * T;
+  return index < count;
 }
 
 // A walked tile in the LDS: rows of DP elements, padded to a power of two of bytes, 16-byte pieces XOR-ed with bits of the row so that
@@ -298,7 +326,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attention_fwd(Args a) {
   __shared__ __attribute__((aligned(16))) char lds[4 * S::TILE];        // keys and values, two tiles in turn
   const int head = blockIdx.x % a.heads;
   Tile t;
-  if (!find_tile<S::OWN>(a, blockIdx.x / a.heads, t)) return;
+  if (!find_tile<S::OWN, false>(a, blockIdx.x / a.heads, t)) return;
   const int kv = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, half = lane >> 5;
   const __bf16* k = a.k + t.first * a.k_row + kv * a.k_head;
   const __bf16* v = a.v + t.first * a.v_row + kv * a.v_head;
@@ -306,43 +334,38 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attention_fwd(Args a) {
   Stage<DP, S::WALK, S::THREADS> sk, sv;
   sk.init(a.k_row, a.head_dim);
   sv.init(a.v_row, a.head_dim);
-#pragma nounroll
-  for (int tile = t.other;; tile = t.index) {
-    const int row = tile * S::OWN;
-    const int first = row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
-    sk.fetch(k, a.k_row, t.len, a.head_dim);
-    sv.fetch(v, a.v_row, t.len, a.head_dim);
-    Forward<DP> f;
-    f.q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, mine < t.len, a.head_dim);
+  const int row = t.row, first = row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
+  sk.fetch(k, a.k_row, t.len, a.head_dim);
+  sv.fetch(v, a.v_row, t.len, a.head_dim);
+  Forward<DP> f;
+  f.q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, mine < t.len, a.head_dim);
 #pragma unroll
-    for (int m = 0; m < DP / 32; ++m) f.acc[m] = zeros16();
-    const int end = a.causal && row + S::OWN < t.len ? row + S::OWN : t.len;          // keys that the workgroup sees
-    const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;      // and this wave
-    const int last = a.causal && mine < t.len ? mine : t.len - 1;                     // the lane's last key
-    const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;              // keys before this one need no mask
-    sk.put(lds);
-    sv.put(lds + S::TILE);
-    __syncthreads();
-    for (int j = 0, turn = 0; j < end; j += S::WALK, turn ^= 2 * S::TILE) {
-      const bool more = j + S::WALK < end;
-      if (more) {
-        sk.fetch(k + (int64_t)(j + S::WALK) * a.k_row, a.k_row, t.len - j - S::WALK, a.head_dim);
-        sv.fetch(v + (int64_t)(j + S::WALK) * a.v_row, a.v_row, t.len - j - S::WALK, a.head_dim);
-      }
-      const char *lds_k = lds + turn, *lds_v = lds_k + S::TILE;
-      if (j < seen) f.template step<S::WALK / 32>(lds_k, lds_v, j, j + S::WALK > whole, last, c);
-      if (more) {
-        sk.put(lds + (turn ^ 2 * S::TILE));
-        sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
-      }
-      __syncthreads();
+  for (int m = 0; m < DP / 32; ++m) f.acc[m] = zeros16();
+  const int end = a.causal && row + S::OWN < t.len ? row + S::OWN : t.len;          // keys that the workgroup sees
+  const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;      // and this wave
+  const int last = a.causal && mine < t.len ? mine : t.len - 1;                     // the lane's last key
+  const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;              // keys before this one need no mask
+  sk.put(lds);
+  sv.put(lds + S::TILE);
+  __syncthreads();
+  for (int j = 0, turn = 0; j < end; j += S::WALK, turn ^= 2 * S::TILE) {
+    const bool more = j + S::WALK < end;
+    if (more) {
+      sk.fetch(k + (int64_t)(j + S::WALK) * a.k_row, a.k_row, t.len - j - S::WALK, a.head_dim);
+      sv.fetch(v + (int64_t)(j + S::WALK) * a.v_row, a.v_row, t.len - j - S::WALK, a.head_dim);
     }
-    f.total += other_half(f.total);
-    const bool there = mine < t.len;
-    store_row<DP>(a.out + (t.first + mine) * a.o_row + head * a.o_head, f.acc, 1.f / f.total, a.head_dim, there);
-    if (there && half == 0) a.lse[head * a.tokens + t.first + mine] = f.top * a.scale + __builtin_amdgcn_logf(f.total) * LN2;
-    if (tile == t.index) break;
+    const char *lds_k = lds + turn, *lds_v = lds_k + S::TILE;
+    if (j < seen) f.template step<S::WALK / 32>(lds_k, lds_v, j, j + S::WALK > whole, last, c);
+    if (more) {
+      sk.put(lds + (turn ^ 2 * S::TILE));
+      sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
+    }
+    __syncthreads();
   }
+  f.total += other_half(f.total);
+  const bool there = mine < t.len;
+  store_row<DP>(a.out + (t.first + mine) * a.o_row + head * a.o_head, f.acc, 1.f / f.total, a.head_dim, there);
+  if (there && half == 0) a.lse[head * a.tokens + t.first + mine] = f.top * a.scale + __builtin_amdgcn_logf(f.total) * LN2;
 }
 
 // dq, and delta = <do, o> of every row for the kernel of dk and dv, which runs after this one.
@@ -352,7 +375,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attention_bwd_q(Args a) {
   __shared__ __attribute__((aligned(16))) char lds[4 * S::TILE];
   const int head = blockIdx.x % a.heads;
   Tile t;
-  if (!find_tile<S::OWN>(a, blockIdx.x / a.heads, t)) return;
+  if (!find_tile<S::OWN, false>(a, blockIdx.x / a.heads, t)) return;
   const int kv = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, half = lane >> 5;
   const __bf16* k = a.k + t.first * a.k_row + kv * a.k_head;
   const __bf16* v = a.v + t.first * a.v_row + kv * a.v_head;
@@ -360,72 +383,67 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attention_bwd_q(Args a) {
   Stage<DP, S::WALK, S::THREADS> sk, sv;
   sk.init(a.k_row, a.head_dim);
   sv.init(a.v_row, a.head_dim);
-#pragma nounroll
-  for (int tile = t.other;; tile = t.index) {
-    const int row = tile * S::OWN;
-    const int first = row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
-    const bool there = mine < t.len;
-    sk.fetch(k, a.k_row, t.len, a.head_dim);
-    sv.fetch(v, a.v_row, t.len, a.head_dim);
-    Rows<DP> q, dout;
-    q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, there, a.head_dim);
-    dout.fetch(a.dout + (t.first + mine) * a.o_row + head * a.o_head, there, a.head_dim);
-    float delta = 0.f;
-    {
-      Rows<DP> o;
-      o.fetch(a.o + (t.first + mine) * a.o_row + head * a.o_head, there, a.head_dim);
+  const int row = t.row, first = row + 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = first + (lane & 31);
+  const bool there = mine < t.len;
+  sk.fetch(k, a.k_row, t.len, a.head_dim);
+  sv.fetch(v, a.v_row, t.len, a.head_dim);
+  Rows<DP> q, dout;
+  q.fetch(a.q + (t.first + mine) * a.q_row + head * a.q_head, there, a.head_dim);
+  dout.fetch(a.dout + (t.first + mine) * a.o_row + head * a.o_head, there, a.head_dim);
+  float delta = 0.f;
+  {
+    Rows<DP> o;
+    o.fetch(a.o + (t.first + mine) * a.o_row + head * a.o_head, there, a.head_dim);
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s)
+    for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) delta = fmaf((float)o.f[s][e], (float)dout.f[s][e], delta);
-      delta += other_half(delta);
-    }
-    const int64_t at = head * a.tokens + t.first + mine;
-    if (there && half == 0) a.delta[at] = delta;
-    const float lse2 = there ? a.lse[at] * LOG2E : 0.f;
-    const int end = a.causal && row + S::OWN < t.len ? row + S::OWN : t.len;
-    const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;
-    const int last = a.causal && there ? mine : t.len - 1;
-    const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;
-    f32x16 acc[DP / 32];
-#pragma unroll
-    for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
-    sk.put(lds);
-    sv.put(lds + S::TILE);
-    __syncthreads();
-    for (int j0 = 0, turn = 0; j0 < end; j0 += S::WALK, turn ^= 2 * S::TILE) {
-      const bool more = j0 + S::WALK < end;
-      if (more) {
-        sk.fetch(k + (int64_t)(j0 + S::WALK) * a.k_row, a.k_row, t.len - j0 - S::WALK, a.head_dim);
-        sv.fetch(v + (int64_t)(j0 + S::WALK) * a.v_row, a.v_row, t.len - j0 - S::WALK, a.head_dim);
-      }
-#pragma unroll
-      for (int sub = 0; sub < S::WALK; sub += 32) {
-        const int j = j0 + sub;
-        if (j >= seen) break;
-        const char* lds_k = lds + turn + sub * Layout<DP>::PITCH;
-        f32x16 s[2];                                                  // scores, and dP
-        products<DP, 2, S::TILE>(s, lds_k, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
-        if (j + 32 > whole) {
-          int most = last - j - 4 * half;
-          asm volatile("" : "+v"(most));
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (walked(r, 0) > most) s[0][r] = -INFINITY;
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2)) * (s[1][r] - delta);
-        accumulate<DP, 1, 0>({&acc}, lds_k, {rounded(s[0])});
-      }
-      if (more) {
-        sk.put(lds + (turn ^ 2 * S::TILE));
-        sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
-      }
-      __syncthreads();
-    }
-    store_row<DP>(a.dq + (t.first + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, there);
-    if (tile == t.index) break;
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)o.f[s][e], (float)dout.f[s][e], delta);
+    delta += other_half(delta);
   }
+  const int64_t at = head * a.tokens + t.first + mine;
+  if (there && half == 0) a.delta[at] = delta;
+  const float lse2 = there ? a.lse[at] * LOG2E : 0.f;
+  const int end = a.causal && row + S::OWN < t.len ? row + S::OWN : t.len;
+  const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;
+  const int last = a.causal && there ? mine : t.len - 1;
+  const int whole = a.causal && first < t.len - 1 ? first + 1 : t.len;
+  f32x16 acc[DP / 32];
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
+  sk.put(lds);
+  sv.put(lds + S::TILE);
+  __syncthreads();
+  for (int j0 = 0, turn = 0; j0 < end; j0 += S::WALK, turn ^= 2 * S::TILE) {
+    const bool more = j0 + S::WALK < end;
+    if (more) {
+      sk.fetch(k + (int64_t)(j0 + S::WALK) * a.k_row, a.k_row, t.len - j0 - S::WALK, a.head_dim);
+      sv.fetch(v + (int64_t)(j0 + S::WALK) * a.v_row, a.v_row, t.len - j0 - S::WALK, a.head_dim);
+    }
+#pragma unroll
+    for (int sub = 0; sub < S::WALK; sub += 32) {
+      const int j = j0 + sub;
+      if (j >= seen) break;
+      const char* lds_k = lds + turn + sub * Layout<DP>::PITCH;
+      f32x16 s[2];                                                  // scores, and dP
+      products<DP, 2, S::TILE>(s, lds_k, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
+      if (j + 32 > whole) {
+        int most = last - j - 4 * half;
+        asm volatile("" : "+v"(most));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (walked(r, 0) > most) s[0][r] = -INFINITY;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2)) * (s[1][r] - delta);
+      accumulate<DP, 1, 0>({&acc}, lds_k, {rounded(s[0])});
+    }
+    if (more) {
+      sk.put(lds + (turn ^ 2 * S::TILE));
+      sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
+    }
+    __syncthreads();
+  }
+  store_row<DP>(a.dq + (t.first + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, there);
 }
 
 // One set of accumulators from the waves of one group to those of the other, which add it to theirs: rows of 16 bytes a lane.
@@ -464,7 +482,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_attention_bwd_kv(Arg
   static_assert(GROUPS == 1 || 2 * BOTH >= WAVES * 64 * DP / 2 * 4);
   const int kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads;
   Tile t;
-  if (!find_tile<OWN>(a, blockIdx.x / a.kv_heads, t)) return;
+  if (!find_tile<OWN, true>(a, blockIdx.x / a.kv_heads, t)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES;
   const int set = GROUPS == 1 ? 0 : (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES;
   const float c = a.scale * LOG2E;
@@ -472,98 +490,94 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_attention_bwd_kv(Arg
   sq.init(a.q_row, a.head_dim);
   so.init(a.o_row, a.head_dim);
   float next_lse = 0.f, next_delta = 0.f;
-#pragma nounroll
-  for (int tile = t.index;; tile = t.other) {
-    const int row = tile * OWN, first = row + 32 * wave, mine = first + (lane & 31);
-    const bool there = mine < t.len;
-    const int begin = a.causal ? row : 0;                            // the first walked query
-    int head = kv * group, i = begin, next = begin;                  // what is fetched next, and the rows under way
-    auto fetch = [&] {
-      const int64_t from = t.first + i;
-      sq.fetch(a.q + from * a.q_row + head * a.q_head, a.q_row, t.len - i, a.head_dim);
-      so.fetch(a.dout + from * a.o_row + head * a.o_head, a.o_row, t.len - i, a.head_dim);
-      next = i;
-      if (threadIdx.x < WALK) {
-        const int64_t at = head * a.tokens + t.first + (i + (int)threadIdx.x < t.len ? i + (int)threadIdx.x : t.len - 1);
-        next_lse = a.lse[at];
-        next_delta = a.delta[at];
-      }
-      i += WALK;
-      if (i >= t.len) { i = begin; ++head; }
-    };
-    auto put = [&](char* to) {
-      sq.put(to);
-      so.put(to + TILE);
-      if (threadIdx.x < WALK) {
-        // rows past the last: exp2(-inf) = 0
-        reinterpret_cast<float*>(to + 2 * TILE)[threadIdx.x] = next + (int)threadIdx.x < t.len ? next_lse * LOG2E : INFINITY;
-        reinterpret_cast<float*>(to + 2 * TILE)[WALK + threadIdx.x] = next_delta;
-      }
-    };
-    fetch();
-    char* const own_v = lds_v + SUB * wave;
-    Rows<DP> k, v;
-    k.fetch(a.k + (t.first + mine) * a.k_row + kv * a.k_head, there, a.head_dim);
-    v.fetch(a.v + (t.first + mine) * a.v_row + kv * a.v_head, there, a.head_dim);
-    if (V_IN_LDS && set == 0) {
-#pragma unroll
-      for (int s = 0; s < DP / 16; ++s) *reinterpret_cast<bf16x8*>(own_v + Layout<DP>::at(lane & 31, 2 * s + half)) = v.f[s];
+  const int row = t.row, first = row + 32 * wave, mine = first + (lane & 31);
+  const bool there = mine < t.len;
+  const int begin = a.causal ? row : 0;                            // the first walked query
+  int head = kv * group, i = begin, next = begin;                  // what is fetched next, and the rows under way
+  auto fetch = [&] {
+    const int64_t from = t.first + i;
+    sq.fetch(a.q + from * a.q_row + head * a.q_head, a.q_row, t.len - i, a.head_dim);
+    so.fetch(a.dout + from * a.o_row + head * a.o_head, a.o_row, t.len - i, a.head_dim);
+    next = i;
+    if (threadIdx.x < WALK) {
+      const int64_t at = head * a.tokens + t.first + (i + (int)threadIdx.x < t.len ? i + (int)threadIdx.x : t.len - 1);
+      next_lse = a.lse[at];
+      next_delta = a.delta[at];
     }
-    f32x16 dk[DP / 32], dv[DP / 32];
-#pragma unroll
-    for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
-    put(lds);
-    __syncthreads();
-    int at = begin;                                                  // what is used now
-    for (int n = (t.len - begin + WALK - 1) / WALK * group, turn = 0; n > 0; --n, turn ^= 1) {
-      const char* const now = lds + turn * BOTH;
-      if (n > 1) fetch();
-      const int from = at + 32 * set;
-      if (first < t.len && from < t.len && !(a.causal && from + 32 <= first)) {
-        f32x16 s[2];                                                  // scores, and dP
-        products<DP, 2, TILE>(s, now + set * SUB, [&](int which, int p, int base) {
-          if (!which) return k.f[p];
-          return V_IN_LDS ? *reinterpret_cast<const bf16x8*>(own_v + (base ^ p << 5)) : v.f[p];
-        });
-        if (a.causal && from < first + 31) {
-          int least = mine - from - 4 * half;
-          asm volatile("" : "+v"(least));
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (walked(r, 0) < least) s[0][r] = -INFINITY;
-        }
-        const float* scalars = reinterpret_cast<const float*>(now + 2 * TILE) + 32 * set + 4 * half;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 l = *reinterpret_cast<const f32x4*>(scalars + 8 * g), d = *reinterpret_cast<const f32x4*>(scalars + WALK + 8 * g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 4 * g + e;
-            s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
-            s[1][r] = s[0][r] * (s[1][r] - d[e]);
-          }
-        }
-        accumulate<DP, 2, TILE>({&dk, &dv}, now + set * SUB, {rounded(s[1]), rounded(s[0])});
-      }
-      at += WALK;
-      if (at >= t.len) at = begin;
-      if (n > 1) put(lds + (turn ^ 1) * BOTH);
-      __syncthreads();
+    i += WALK;
+    if (i >= t.len) { i = begin; ++head; }
+  };
+  auto put = [&](char* to) {
+    sq.put(to);
+    so.put(to + TILE);
+    if (threadIdx.x < WALK) {
+      // rows past the last: exp2(-inf) = 0
+      reinterpret_cast<float*>(to + 2 * TILE)[threadIdx.x] = next + (int)threadIdx.x < t.len ? next_lse * LOG2E : INFINITY;
+      reinterpret_cast<float*>(to + 2 * TILE)[WALK + threadIdx.x] = next_delta;
     }
-    if (GROUPS == 2) {
-      if (set) hand_over<DP>(lds, wave, dk);
-      __syncthreads();
-      if (!set) take_over<DP>(lds, wave, dk);
-      __syncthreads();
-      if (!set) hand_over<DP>(lds, wave, dv);
-      __syncthreads();
-      if (set) take_over<DP>(lds, wave, dv);
-      __syncthreads();
-    }
-    if (!set) store_row<DP>(a.dk + (t.first + mine) * a.k_row + kv * a.k_head, dk, a.scale, a.head_dim, there);
-    if (GROUPS == 1 || set) store_row<DP>(a.dv + (t.first + mine) * a.v_row + kv * a.v_head, dv, 1.f, a.head_dim, there);
-    if (tile == t.other) break;
+  };
+  fetch();
+  char* const own_v = lds_v + SUB * wave;
+  Rows<DP> k, v;
+  k.fetch(a.k + (t.first + mine) * a.k_row + kv * a.k_head, there, a.head_dim);
+  v.fetch(a.v + (t.first + mine) * a.v_row + kv * a.v_head, there, a.head_dim);
+  if (V_IN_LDS && set == 0) {
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) *reinterpret_cast<bf16x8*>(own_v + Layout<DP>::at(lane & 31, 2 * s + half)) = v.f[s];
   }
+  f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
+  put(lds);
+  __syncthreads();
+  int at = begin;                                                  // what is used now
+  for (int n = (t.len - begin + WALK - 1) / WALK * group, turn = 0; n > 0; --n, turn ^= 1) {
+    const char* const now = lds + turn * BOTH;
+    if (n > 1) fetch();
+    const int from = at + 32 * set;
+    if (first < t.len && from < t.len && !(a.causal && from + 32 <= first)) {
+      f32x16 s[2];                                                  // scores, and dP
+      products<DP, 2, TILE>(s, now + set * SUB, [&](int which, int p, int base) {
+        if (!which) return k.f[p];
+        return V_IN_LDS ? *reinterpret_cast<const bf16x8*>(own_v + (base ^ p << 5)) : v.f[p];
+      });
+      if (a.causal && from < first + 31) {
+        int least = mine - from - 4 * half;
+        asm volatile("" : "+v"(least));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (walked(r, 0) < least) s[0][r] = -INFINITY;
+      }
+      const float* scalars = reinterpret_cast<const float*>(now + 2 * TILE) + 32 * set + 4 * half;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 l = *reinterpret_cast<const f32x4*>(scalars + 8 * g), d = *reinterpret_cast<const f32x4*>(scalars + WALK + 8 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * g + e;
+          s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
+          s[1][r] = s[0][r] * (s[1][r] - d[e]);
+        }
+      }
+      accumulate<DP, 2, TILE>({&dk, &dv}, now + set * SUB, {rounded(s[1]), rounded(s[0])});
+    }
+    at += WALK;
+    if (at >= t.len) at = begin;
+    if (n > 1) put(lds + (turn ^ 1) * BOTH);
+    __syncthreads();
+  }
+  if (GROUPS == 2) {
+    if (set) hand_over<DP>(lds, wave, dk);
+    __syncthreads();
+    if (!set) take_over<DP>(lds, wave, dk);
+    __syncthreads();
+    if (!set) hand_over<DP>(lds, wave, dv);
+    __syncthreads();
+    if (set) take_over<DP>(lds, wave, dv);
+    __syncthreads();
+  }
+  if (!set) store_row<DP>(a.dk + (t.first + mine) * a.k_row + kv * a.k_head, dk, a.scale, a.head_dim, there);
+  if (GROUPS == 1 || set) store_row<DP>(a.dv + (t.first + mine) * a.v_row + kv * a.v_head, dv, 1.f, a.head_dim, there);
 }
 
 int check(const disco_attention_shape* s) {
