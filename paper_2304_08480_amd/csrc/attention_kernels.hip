@@ -181,6 +181,21 @@ __device__ __forceinline__ f32x16 zeros16() {
   return z;
 }
 
+// The order in which a block's LDS reads and matrix instructions are to be issued: AHEAD reads first, then MFMAS instructions with READS reads after
+// each as long as there are any.  Left alone the compiler reads an operand just before its use, and every product waits for the LDS.
+constexpr int AHEAD_P = 6, AHEAD_A = 8;
+template <int AHEAD, int READS, int TOTAL, int MFMAS>
+__device__ __forceinline__ void interleave() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD < TOTAL ? AHEAD : TOTAL, 0);
+  constexpr int STEPS = AHEAD < TOTAL ? (TOTAL - AHEAD) / READS : 0;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, MFMAS - STEPS, 0);
+}
+
 // 32 walked rows times the lanes' rows: element r of a lane is walked row 8 (r / 4) + 4 half + r % 4.  N such products at once, c[n] of
 // the rows at lds + n STEP with b(n, s): they share the addresses, and no product waits for the one before it.  (The lane's address is hidden from the
 // compiler: it would keep one register for each of the DP / 16 pieces, 16 more in accumulate(), and have none left for two waves a SIMD.)
@@ -196,6 +211,7 @@ __device__ __forceinline__ void products(f32x16 (&c)[N], const char* lds, B b) {
 #pragma unroll
     for (int n = 0; n < N; ++n) c[n] = mfma(*reinterpret_cast<const bf16x8*>(at + n * STEP), b(n, s, base), s ? c[n] : zeros16());
   }
+  interleave<AHEAD_P, 1, DP / 16 * N, DP / 16 * N>();
 }
 __device__ __forceinline__ int walked(int r, int half) { return 8 * (r >> 2) + 4 * half + (r & 3); }
 
@@ -229,6 +245,7 @@ __device__ __forceinline__ void accumulate(f32x16 (*const (&acc)[N])[DP / 32], c
         (*acc[n])[m] = mfma(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), w[n].f[j], (*acc[n])[m]);
       }
   }
+  interleave<AHEAD_A, 2, DP / 32 * 4 * N, DP / 32 * 2 * N>();
 }
 
 // A lane's row of an accumulated product, times f, as bf16.  The two halves of a wave hold 4 channels each of every 8 of a row: they exchange
