@@ -42,6 +42,7 @@ struct Args {
   __bf16 *out, *dq, *dk, *dv;
   float *lse, *delta;
   int32_t slots;
+  int32_t above;                // sequences of up to this many rows are another kernel's
 };
 
 // Which tile of T rows of which sequence a workgroup has.  Causal: tile i of queries has i + 1 tiles of keys to walk, the i-th last tile of keys
@@ -63,7 +64,7 @@ __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
   int from, len, index;
   if (a.sequences <= 64) {
     const bool there = lane < a.sequences;
-    const int first = there ? start(lane) : 0, mine = there ? start(lane + 1) - first : 0, tiles = mine > 0 ? (mine - 1) / T + 1 : 0;
+    const int first = there ? start(lane) : 0, mine = there ? start(lane + 1) - first : 0, tiles = mine > a.above ? (mine - 1) / T + 1 : 0;
     auto later = [&](int k) { return wave_reduce(tiles >= k ? tiles - k + 1 : 0, [](int x, int y) { return x + y; }); };
     if (slot >= later(1)) return false;
     int k = 1, over = wave_reduce(tiles, [](int x, int y) { return x > y ? x : y; }) + 1, before = 0;      // N(k) > slot >= N(over) = before
@@ -101,7 +102,15 @@ __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
   t.first = from;
   t.len = len;
   t.row = (KEYS && a.causal ? count - 1 - index : index) * T;
-  return index < count;
+  return index < count && len > a.above;
+}
+
+// Whether any sequence is left to the kernels that follow those for short sequences: they are launched before that is known, as few workgroups, and
+// mostly end here.
+__device__ __forceinline__ bool any_rest(const Args& a) {
+  bool any = false;
+  for (int s = threadIdx.x; s < a.sequences; s += blockDim.x) any |= a.starts[s + 1] - a.starts[s] > a.above;
+  return __syncthreads_or(any);
 }
 
 // A walked tile in the LDS: rows of DP elements, padded to a power of two of bytes, 16-byte pieces XOR-ed with bits of the row so that
@@ -140,7 +149,7 @@ struct Stage {
   __device__ __forceinline__ void init(int64_t pitch, int head_dim) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int id = threadIdx.x + i * THREADS, row = id / L::PIECES, piece = id % L::PIECES;
+      const int id = threadIdx.x % THREADS + i * THREADS, row = id / L::PIECES, piece = id % L::PIECES;
       from[i] = piece * 8 < head_dim && row < ROWS ? (uint32_t)row * (uint32_t)(pitch * 2) + piece * 16 : NOWHERE;
     }
   }
@@ -152,7 +161,7 @@ struct Stage {
   __device__ __forceinline__ void put(char* lds) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int id = threadIdx.x + i * THREADS;
+      const int id = threadIdx.x % THREADS + i * THREADS;
       if (ALL % THREADS == 0 || id < ALL) *reinterpret_cast<u32x4*>(lds + L::at(id / L::PIECES, id % L::PIECES)) = v[i];
     }
   }
@@ -338,12 +347,8 @@ struct Forward {
 };
 
 template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_attention_fwd(Args a) {
+__device__ __forceinline__ void forward_tile(const Args& a, const Tile& t, int head, char* lds) {
   using S = Shape<DP, WAVES>;
-  __shared__ __attribute__((aligned(16))) char lds[4 * S::TILE];        // keys and values, two tiles in turn
-  const int head = blockIdx.x % a.heads;
-  Tile t;
-  if (!find_tile<S::OWN, false>(a, blockIdx.x / a.heads, t)) return;
   const int kv = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, half = lane >> 5;
   const __bf16* k = a.k + t.first * a.k_row + kv * a.k_head;
   const __bf16* v = a.v + t.first * a.v_row + kv * a.v_head;
@@ -385,14 +390,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attention_fwd(Args a) {
   if (there && half == 0) a.lse[head * a.tokens + t.first + mine] = f.top * a.scale + __builtin_amdgcn_logf(f.total) * LN2;
 }
 
+template <int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attention_fwd(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[4 * Shape<DP, WAVES>::TILE];        // keys and values, two tiles in turn
+  Tile t;
+  if (find_tile<32 * WAVES, false>(a, blockIdx.x / a.heads, t)) forward_tile<DP, WAVES>(a, t, blockIdx.x % a.heads, lds);
+}
+template <int DP>
+__global__ __launch_bounds__(256, 2) void k_attention_fwd_rest(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[4 * Shape<DP, 4>::TILE];
+  if (!any_rest(a)) return;
+  Tile t;
+#pragma nounroll
+  for (int slot = blockIdx.x / a.heads; slot < a.slots; slot += gridDim.x / a.heads)
+    if (find_tile<128, false>(a, slot, t)) forward_tile<DP, 4>(a, t, blockIdx.x % a.heads, lds);
+}
+
 // dq, and delta = <do, o> of every row for the kernel of dk and dv, which runs after this one.
 template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_attention_bwd_q(Args a) {
+__device__ __forceinline__ void queries_tile(const Args& a, const Tile& t, int head, char* lds) {
   using S = Shape<DP, WAVES>;
-  __shared__ __attribute__((aligned(16))) char lds[4 * S::TILE];
-  const int head = blockIdx.x % a.heads;
-  Tile t;
-  if (!find_tile<S::OWN, false>(a, blockIdx.x / a.heads, t)) return;
   const int kv = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, half = lane >> 5;
   const __bf16* k = a.k + t.first * a.k_row + kv * a.k_head;
   const __bf16* v = a.v + t.first * a.v_row + kv * a.v_head;
@@ -463,6 +480,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attention_bwd_q(Args a) {
   store_row<DP>(a.dq + (t.first + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, there);
 }
 
+template <int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attention_bwd_q(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[4 * Shape<DP, WAVES>::TILE];
+  Tile t;
+  if (find_tile<32 * WAVES, false>(a, blockIdx.x / a.heads, t)) queries_tile<DP, WAVES>(a, t, blockIdx.x % a.heads, lds);
+}
+template <int DP>
+__global__ __launch_bounds__(256, 2) void k_attention_bwd_q_rest(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[4 * Shape<DP, 4>::TILE];
+  if (!any_rest(a)) return;
+  Tile t;
+#pragma nounroll
+  for (int slot = blockIdx.x / a.heads; slot < a.slots; slot += gridDim.x / a.heads)
+    if (find_tile<128, false>(a, slot, t)) queries_tile<DP, 4>(a, t, blockIdx.x % a.heads, lds);
+}
+
 // One set of accumulators from the waves of one group to those of the other, which add it to theirs: rows of 16 bytes a lane.
 template <int DP>
 __device__ __forceinline__ void hand_over(char* lds, int wave, const f32x16 (&acc)[DP / 32]) {
@@ -489,17 +522,21 @@ __device__ __forceinline__ void take_over(const char* lds, int wave, f32x16 (&ac
 // WAVES waves.  Two sets share the keys (and the sums, which meet at the end) where the key tiles are no more than the compute units: one sequence of
 // 8192, causal, head width 128, 16 heads on 8 of keys: 630 us against 928 with one set; on 16 of keys, two workgroups of one set a unit, 640 against 585.
 template <int DP, int WAVES, int GROUPS>
-__global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_attention_bwd_kv(Args a) {
-  constexpr int OWN = 32 * WAVES, SUB = 32 * Layout<DP>::PITCH;
-  constexpr int WALK = 32 * GROUPS, TILE = GROUPS * SUB, BOTH = 2 * TILE + 2 * WALK * (int)sizeof(float);      // queries, do, lse, delta
+struct Keys {
+  static constexpr int SUB = 32 * Layout<DP>::PITCH, WALK = 32 * GROUPS, TILE = GROUPS * SUB;
+  static constexpr int BOTH = 2 * TILE + 2 * WALK * (int)sizeof(float);      // queries, do, lse, delta
   // Wide heads: the accumulators of dk and dv take 2 DP registers a lane, k and v another DP; with v in the LDS two waves fit a SIMD.
-  constexpr bool V_IN_LDS = DP > 64;
-  __shared__ __attribute__((aligned(16))) char lds[2 * BOTH];
-  __shared__ __attribute__((aligned(16))) char lds_v[V_IN_LDS ? OWN * Layout<DP>::PITCH : 16];
+  static constexpr bool V_IN_LDS = DP > 64;
+  static constexpr int ALL = 2 * BOTH + (V_IN_LDS ? WAVES * SUB : 0);
   static_assert(GROUPS == 1 || 2 * BOTH >= WAVES * 64 * DP / 2 * 4);
-  const int kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads;
-  Tile t;
-  if (!find_tile<OWN, true>(a, blockIdx.x / a.kv_heads, t)) return;
+};
+template <int DP, int WAVES, int GROUPS>
+__device__ __forceinline__ void keys_tile(const Args& a, const Tile& t, int kv, char* lds) {
+  using S = Keys<DP, WAVES, GROUPS>;
+  constexpr int SUB = S::SUB, WALK = S::WALK, TILE = S::TILE, BOTH = S::BOTH;
+  constexpr bool V_IN_LDS = S::V_IN_LDS;
+  char* const lds_v = lds + 2 * BOTH;
+  const int group = a.heads / a.kv_heads;
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES;
   const int set = GROUPS == 1 ? 0 : (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES;
   const float c = a.scale * LOG2E;
@@ -597,6 +634,202 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_attention_bwd_kv(Arg
   if (GROUPS == 1 || set) store_row<DP>(a.dv + (t.first + mine) * a.v_row + kv * a.v_head, dv, 1.f, a.head_dim, there);
 }
 
+template <int DP, int WAVES, int GROUPS>
+__global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_attention_bwd_kv(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[Keys<DP, WAVES, GROUPS>::ALL];
+  Tile t;
+  if (find_tile<32 * WAVES, true>(a, blockIdx.x / a.kv_heads, t)) keys_tile<DP, WAVES, GROUPS>(a, t, blockIdx.x % a.kv_heads, lds);
+}
+template <int DP>
+__global__ __launch_bounds__(256, 2) void k_attention_bwd_kv_rest(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[Keys<DP, 4, 1>::ALL];
+  if (!any_rest(a)) return;
+  Tile t;
+#pragma nounroll
+  for (int slot = blockIdx.x / a.kv_heads; slot < a.slots; slot += gridDim.x / a.kv_heads)
+    if (find_tile<128, true>(a, slot, t)) keys_tile<DP, 4, 1>(a, t, blockIdx.x % a.kv_heads, lds);
+}
+
+// ---- Short sequences: a workgroup has all of one, WAVES tiles of 32 rows at most, for one head.  Every row is read from memory once and kept by its
+// wave, 16 bytes a lane at a time, which is also how it goes into the LDS for the other waves; there is no walk to be kept supplied, no search for
+// the tile, and the backward pass is one kernel: the queries' side first, then the waves put queries and do in the place of keys and values.
+template <int DP, int WAVES>
+struct Short {
+  static constexpr int ROWS = 32 * WAVES, SUB = 32 * Layout<DP>::PITCH, ALL = WAVES * SUB;
+};
+// The sequence of a workgroup, if it is one of these and the wave has rows of it.  (A wave without rows ends; the barriers do not wait for it.)
+template <int WAVES>
+__device__ __forceinline__ bool short_sequence(const Args& a, int s, int64_t& first, int& len) {
+  const int tokens = (int)a.tokens, x = a.starts[s], y = a.starts[s + 1];
+  const int from = x < 0 ? 0 : x > tokens ? tokens : x, to = y < 0 ? 0 : y > tokens ? tokens : y;
+  first = from;
+  len = to - from;
+  return len > 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) && len <= 32 * WAVES;
+}
+template <int DP>
+__device__ __forceinline__ void put_rows(char* lds, const Rows<DP>& r) {
+  const int lane = threadIdx.x & 63, base = Layout<DP>::at(lane & 31, lane >> 5);
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) *reinterpret_cast<bf16x8*>(lds + (base ^ s << 5)) = r.f[s];
+}
+
+template <int DP>
+__device__ __forceinline__ void take_rows(const char* lds, Rows<DP>& r) {
+  const int lane = threadIdx.x & 63, base = Layout<DP>::at(lane & 31, lane >> 5);
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) r.f[s] = *reinterpret_cast<const bf16x8*>(lds + (base ^ s << 5));
+}
+
+template <int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void k_attention_fwd_short(Args a) {
+  using S = Short<DP, WAVES>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * S::ALL];
+  const int head = blockIdx.x % a.heads, kv = head / (a.heads / a.kv_heads);
+  int64_t seq;
+  int len;
+  if (!short_sequence<WAVES>(a, blockIdx.x / a.heads, seq, len)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, mine = 32 * wave + (lane & 31);
+  const bool there = mine < len;
+  Forward<DP> f;
+  {
+    Stage<DP, 32, 64> q, k, v;
+    q.init(a.q_row, a.head_dim);
+    k.init(a.k_row, a.head_dim);
+    v.init(a.v_row, a.head_dim);
+    const int64_t row = seq + 32 * wave;
+    const int rows = len - 32 * wave;
+    q.fetch(a.q + row * a.q_row + head * a.q_head, a.q_row, rows, a.head_dim);
+    k.fetch(a.k + row * a.k_row + kv * a.k_head, a.k_row, rows, a.head_dim);
+    v.fetch(a.v + row * a.v_row + kv * a.v_head, a.v_row, rows, a.head_dim);
+    char *own = lds + wave * S::SUB;
+    q.put(own);
+    take_rows<DP>(own, f.q);
+    k.put(own);
+    v.put(own + S::ALL);
+  }
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m) f.acc[m] = zeros16();
+  const float c = a.scale * LOG2E;
+  const int last = a.causal && there ? mine : len - 1, tiles = a.causal ? wave + 1 : (len + 31) / 32;
+  __syncthreads();
+  for (int t = 0; t < tiles; ++t)
+    f.template step<1>(lds + t * S::SUB, lds + S::ALL + t * S::SUB, 32 * t, (a.causal && t == wave) || 32 * t + 32 > len, last, c);
+  f.total += other_half(f.total);
+  store_row<DP>(a.out + (seq + mine) * a.o_row + head * a.o_head, f.acc, 1.f / f.total, a.head_dim, there);
+  if (there && half == 0) a.lse[head * a.tokens + seq + mine] = f.top * a.scale + __builtin_amdgcn_logf(f.total) * LN2;
+}
+
+// heads == kv_heads
+template <int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void k_attention_bwd_short(Args a) {
+  using S = Short<DP, WAVES>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * S::ALL];
+  __shared__ __attribute__((aligned(16))) float row_lse[S::ROWS], row_delta[S::ROWS];
+  const int head = blockIdx.x % a.heads;
+  int64_t seq;
+  int len;
+  if (!short_sequence<WAVES>(a, blockIdx.x / a.heads, seq, len)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, mine = 32 * wave + (lane & 31);
+  const bool there = mine < len;
+  const int tiles = (len + 31) / 32;
+  const float c = a.scale * LOG2E;
+  Rows<DP> q, dout, k, v;
+  const float lse2 = there ? a.lse[head * a.tokens + seq + mine] * LOG2E : INFINITY;      // exp2(-inf) = 0
+  float delta = 0.f;
+  {
+    Stage<DP, 32, 64> sq, sk, sv, so, sd;
+    sq.init(a.q_row, a.head_dim);
+    sk.init(a.k_row, a.head_dim);
+    sv.init(a.v_row, a.head_dim);
+    so.init(a.o_row, a.head_dim);
+    sd.init(a.o_row, a.head_dim);
+    const int64_t row = seq + 32 * wave;
+    const int rows = len - 32 * wave;
+    sq.fetch(a.q + row * a.q_row + head * a.q_head, a.q_row, rows, a.head_dim);
+    sd.fetch(a.dout + row * a.o_row + head * a.o_head, a.o_row, rows, a.head_dim);
+    so.fetch(a.o + row * a.o_row + head * a.o_head, a.o_row, rows, a.head_dim);
+    sk.fetch(a.k + row * a.k_row + head * a.k_head, a.k_row, rows, a.head_dim);
+    sv.fetch(a.v + row * a.v_row + head * a.v_head, a.v_row, rows, a.head_dim);
+    char* own = lds + wave * S::SUB;
+    Rows<DP> o;
+    sq.put(own);
+    sd.put(own + S::ALL);
+    take_rows<DP>(own, q);
+    take_rows<DP>(own + S::ALL, dout);
+    so.put(own);
+    take_rows<DP>(own, o);
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)o.f[s][e], (float)dout.f[s][e], delta);
+    delta += other_half(delta);
+    sk.put(own);
+    sv.put(own + S::ALL);
+    take_rows<DP>(own, k);
+    take_rows<DP>(own + S::ALL, v);
+  }
+  __syncthreads();
+  {
+    f32x16 acc[DP / 32];
+#pragma unroll
+    for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
+    const int last = a.causal && there ? mine : len - 1, end = a.causal ? wave + 1 : tiles;
+    for (int t = 0; t < end; ++t) {
+      const char* now = lds + t * S::SUB;
+      f32x16 s[2];                                                  // scores, and dP
+      products<DP, 2, S::ALL>(s, now, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
+      if ((a.causal && t == wave) || 32 * t + 32 > len) {
+        int most = last - 32 * t - 4 * half;
+        asm volatile("" : "+v"(most));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (walked(r, 0) > most) s[0][r] = -INFINITY;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2)) * (s[1][r] - delta);
+      accumulate<DP, 1, 0>({&acc}, now, {rounded(s[0])});
+    }
+    store_row<DP>(a.dq + (seq + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, there);
+  }
+  __syncthreads();
+  put_rows<DP>(lds + wave * S::SUB, q);
+  put_rows<DP>(lds + S::ALL + wave * S::SUB, dout);
+  if (half == 0) {
+    row_lse[mine] = lse2;
+    row_delta[mine] = delta;
+  }
+  __syncthreads();
+  f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
+  for (int t = a.causal ? wave : 0; t < tiles; ++t) {
+    const char* now = lds + t * S::SUB;
+    f32x16 s[2];
+    products<DP, 2, S::ALL>(s, now, [&](int n, int i, int) { return n ? v.f[i] : k.f[i]; });
+    if (a.causal && t == wave) {
+      int least = mine - 32 * t - 4 * half;
+      asm volatile("" : "+v"(least));
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (walked(r, 0) < least) s[0][r] = -INFINITY;
+    }
+    const float *lse = row_lse + 32 * t + 4 * half, *del = row_delta + 32 * t + 4 * half;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 l = *reinterpret_cast<const f32x4*>(lse + 8 * g), d = *reinterpret_cast<const f32x4*>(del + 8 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * g + e;
+        s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
+        s[1][r] = s[0][r] * (s[1][r] - d[e]);
+      }
+    }
+    accumulate<DP, 2, S::ALL>({&dk, &dv}, now, {rounded(s[1]), rounded(s[0])});
+  }
+  store_row<DP>(a.dk + (seq + mine) * a.k_row + head * a.k_head, dk, a.scale, a.head_dim, there);
+  store_row<DP>(a.dv + (seq + mine) * a.v_row + head * a.v_head, dv, 1.f, a.head_dim, there);
+}
+
 int check(const disco_attention_shape* s) {
   if (!s) return DISCO_ERR_NULL;
   if (s->tokens <= 0 || s->tokens > 0x7fffffff || s->sequences <= 0 || s->sequences > 1 << 24 || s->heads <= 0 || s->kv_heads <= 0 ||
@@ -631,30 +864,67 @@ Args args_of(const disco_attention_shape& s, const int32_t* starts) {
 
 constexpr int COMPUTE_UNITS = 256;
 
-int waves_of(const disco_attention_shape& s) { return s.tokens <= (int64_t)96 * s.sequences ? 1 : 4; }
+
+// Tiles of 32 rows that the kernels for short sequences take, 0: none.  The lengths are on the device; the mean says what they may be.
+int short_tiles(const disco_attention_shape& s, bool backward) {
+  if ((backward && s.heads != s.kv_heads) || s.sequences > 8192) return 0;
+  for (int w = 2; w <= 4; ++w)
+    if (s.tokens * 3 <= (int64_t)s.sequences * (32 * w)) return w;
+  const int widest = s.head_dim <= 64 ? 8 : 4;
+  return s.tokens * 5 <= (int64_t)s.sequences * (32 * widest * 4) ? widest : 0;
+}
+template <int DP, class F>
+void with_short(int tiles, F f) {
+  if (tiles == 2) f(std::integral_constant<int, 2>());
+  else if (tiles == 3) f(std::integral_constant<int, 3>());
+  else if (tiles == 4) f(std::integral_constant<int, 4>());
+  else if constexpr (DP <= 64) f(std::integral_constant<int, 8>());
+}
+// The workgroups of a kernel that takes what is left: what the chip holds, whole slots.
+unsigned rest_grid(const Args& a, int heads) {
+  const int64_t slots = (2 * COMPUTE_UNITS + heads - 1) / heads;
+  return (unsigned)((slots < a.slots ? slots : a.slots) * heads);
+}
+bool launched() { return hipGetLastError() == hipSuccess; }
 
 template <int DP, int WAVES>
-bool forward(Args a, hipStream_t st) {
+bool forward(Args a, int tiles, hipStream_t st) {
   a.slots = (int)(a.tokens / (32 * WAVES)) + a.sequences;
-  k_attention_fwd<DP, WAVES><<<(unsigned)(a.slots * a.heads), 64 * WAVES, 0, st>>>(a);
-  return hipGetLastError() == hipSuccess;
+  if (!tiles) {
+    k_attention_fwd<DP, WAVES><<<(unsigned)(a.slots * a.heads), 64 * WAVES, 0, st>>>(a);
+    return launched();
+  }
+  a.above = 32 * tiles;
+  with_short<DP>(tiles, [&](auto w) { k_attention_fwd_short<DP, w()><<<(unsigned)(a.sequences * a.heads), 64 * w(), 0, st>>>(a); });
+  if (!launched() || a.tokens <= a.above) return launched();
+  k_attention_fwd_rest<DP><<<rest_grid(a, a.heads), 256, 0, st>>>(a);
+  return launched();
 }
 template <int DP, int WAVES>
-bool backward(Args a, hipStream_t st) {
+bool backward(Args a, int tiles, hipStream_t st) {
   a.slots = (int)(a.tokens / (32 * WAVES)) + a.sequences;
-  k_attention_bwd_q<DP, WAVES><<<(unsigned)(a.slots * a.heads), 64 * WAVES, 0, st>>>(a);
-  if (hipGetLastError() != hipSuccess) return false;
-  const unsigned grid = (unsigned)(a.slots * a.kv_heads);
-  const int64_t work = a.tokens / (32 * WAVES) * a.kv_heads / (a.causal ? 2 : 1);      // workgroups that have some, nearly
-  if (WAVES == 1 || work > COMPUTE_UNITS) k_attention_bwd_kv<DP, WAVES, 1><<<grid, 64 * WAVES, 0, st>>>(a);
-  else k_attention_bwd_kv<DP, WAVES, WAVES == 1 ? 1 : 2><<<grid, 128 * WAVES, 0, st>>>(a);
-  return hipGetLastError() == hipSuccess;
+  if (!tiles) {
+    k_attention_bwd_q<DP, WAVES><<<(unsigned)(a.slots * a.heads), 64 * WAVES, 0, st>>>(a);
+    if (!launched()) return false;
+    const unsigned grid = (unsigned)(a.slots * a.kv_heads);
+    const int64_t work = a.tokens / (32 * WAVES) * a.kv_heads / (a.causal ? 2 : 1);      // workgroups that have some, nearly
+    if (WAVES == 1 || work > COMPUTE_UNITS) k_attention_bwd_kv<DP, WAVES, 1><<<grid, 64 * WAVES, 0, st>>>(a);
+    else k_attention_bwd_kv<DP, WAVES, WAVES == 1 ? 1 : 2><<<grid, 128 * WAVES, 0, st>>>(a);
+    return launched();
+  }
+  a.above = 32 * tiles;
+  with_short<DP>(tiles, [&](auto w) { k_attention_bwd_short<DP, w()><<<(unsigned)(a.sequences * a.heads), 64 * w(), 0, st>>>(a); });
+  if (!launched() || a.tokens <= a.above) return launched();
+  k_attention_bwd_q_rest<DP><<<rest_grid(a, a.heads), 256, 0, st>>>(a);
+  if (!launched()) return false;
+  k_attention_bwd_kv_rest<DP><<<rest_grid(a, a.kv_heads), 256, 0, st>>>(a);
+  return launched();
 }
 
 // f with the head's width rounded up to a multiple of 32 and the waves of a workgroup as constants
 template <class F>
-int dispatch(const disco_attention_shape& s, F f) {
-  const int dp = (s.head_dim + 31) / 32, waves = waves_of(s);
+int dispatch(const disco_attention_shape& s, int tiles, F f) {
+  const int dp = (s.head_dim + 31) / 32, waves = tiles || s.tokens > (int64_t)96 * s.sequences ? 4 : 1;
 #define DISCO_DP(N) \
   if (dp == N) return (waves == 1 ? f(std::integral_constant<int, 32 * N>(), std::integral_constant<int, 1>()) \
                                   : f(std::integral_constant<int, 32 * N>(), std::integral_constant<int, 4>())) ? DISCO_OK : DISCO_ERR_HIP
@@ -684,7 +954,8 @@ extern "C" int disco_attention_fwd(const disco_attention_shape* shape, const int
   Args a = args_of(*shape, starts);
   a.q = static_cast<const __bf16*>(q); a.k = static_cast<const __bf16*>(k); a.v = static_cast<const __bf16*>(v);
   a.out = static_cast<__bf16*>(o); a.lse = lse;
-  return dispatch(*shape, [&](auto dp, auto waves) { return forward<dp(), waves()>(a, static_cast<hipStream_t>(hip_stream)); });
+  const int tiles = short_tiles(*shape, false);
+  return dispatch(*shape, tiles, [&](auto dp, auto waves) { return forward<dp(), waves()>(a, tiles, static_cast<hipStream_t>(hip_stream)); });
 }
 
 extern "C" int disco_attention_bwd(const disco_attention_shape* shape, const int32_t* starts, const void* q, const void* k, const void* v,
@@ -701,5 +972,6 @@ extern "C" int disco_attention_bwd(const disco_attention_shape* shape, const int
   a.o = static_cast<const __bf16*>(o); a.dout = static_cast<const __bf16*>(dout);
   a.dq = static_cast<__bf16*>(dq); a.dk = static_cast<__bf16*>(dk); a.dv = static_cast<__bf16*>(dv);
   a.lse = const_cast<float*>(lse); a.delta = static_cast<float*>(workspace);
-  return dispatch(*shape, [&](auto dp, auto waves) { return backward<dp(), waves()>(a, static_cast<hipStream_t>(hip_stream)); });
+  const int tiles = short_tiles(*shape, true);
+  return dispatch(*shape, tiles, [&](auto dp, auto waves) { return backward<dp(), waves()>(a, tiles, static_cast<hipStream_t>(hip_stream)); });
 }

@@ -175,3 +175,29 @@ def test_captured_and_on_another_stream():
     torch.cuda.synchronize()
     for x, want in zip((a, b), eager):
         assert all(torch.equal(want[n], y) for n, y in x.outputs().items())
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dim", [32, 64, 88, 128])
+@pytest.mark.parametrize("typical,longer", [(18, 33), (18, 300), (30, 97), (40, 700), (100, 129), (180, 257), (190, 500)])
+def test_many_short_sequences_and_a_few_longer_ones(typical, longer, dim, causal):
+    # sequences of every length around the typical one, in a batch whose mean says short; the longer ones first, amid and last
+    print("case attention mixed", typical, longer, dim, causal, flush=True)
+    g = torch.Generator().manual_seed(typical)
+    n = 70 if typical < 100 else 24
+    lengths = torch.randint(max(0, typical // 3), typical + typical // 3 + 1, (n,), generator=g).tolist()
+    lengths = [longer] + lengths[:n // 2] + [longer, 0] + lengths[n // 2:] + [longer + 1]
+    a = Attention(lengths, 2, 2, dim, causal, seed=dim, behind=3)
+    a.forward()
+    a.backward()
+    a.check()
+
+
+@pytest.mark.parametrize("kv_heads", [1, 2])
+def test_short_sequences_on_both_sides_of_their_limit(kv_heads):
+    for n in (8192, 8193):
+        g = torch.Generator().manual_seed(n)
+        a = Attention(torch.randint(0, 5, (n,), generator=g).tolist(), 2, kv_heads, 32, True, seed=n)
+        a.forward()
+        a.backward()
+        a.check()
