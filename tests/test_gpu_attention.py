@@ -201,3 +201,17 @@ def test_short_sequences_on_both_sides_of_their_limit(kv_heads):
         a.forward()
         a.backward()
         a.check()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (3, 1, 128), (4, 2, 32), (8, 2, 96), (20, 2, 64), (20, 20, 64), (20, 20, 128)])
+def test_long_sequences_on_few_and_many_heads(heads, kv_heads, dim, causal):
+    print("case attention long", heads, kv_heads, dim, causal, flush=True)
+    a = Attention([1100, 3, 900, 97], heads, kv_heads, dim, causal, seed=heads)
+    a.forward()
+    a.backward()
+    a.check()
+    one = a.outputs()
+    a.forward()
+    a.backward()
+    assert all(torch.equal(one[n], x) for n, x in a.outputs().items())
