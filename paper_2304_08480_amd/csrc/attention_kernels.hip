@@ -51,7 +51,8 @@ struct Args {
 //
 // Up to 64 sequences: the tiles with the most to do first, so that the workgroups that take longest are not the last to start.  A lane has a
 // sequence; N(k), the number of tiles that are the k-th or a later one of their sequence (that have at least k to do), falls with k, and slot n's tile has the
-// largest k with N(k) > n.  (24 documents of 1 to 2048 tokens, 16 heads of 128, forward: PAIRED us, LONGEST.)
+// largest k with N(k) > n.  (24 documents of 1 to 2048 tokens, 16 heads of 128, forward: 118 us;
+// sequence by sequence, a tile and its mirror image together so that all are equal, 138.)
 //
 // More: sequence s owns the slots from starts[s] / T + s on, at least as many as it has tiles, whatever its start, so the tiles are found with no table
 // and no count of them, for at most `sequences` idle workgroups more.  The search is 64 ways wide: two rounds of loads for thousands of sequences.
@@ -930,10 +931,19 @@ bool launched() { return hipGetLastError() == hipSuccess; }
 // Sets of waves that share rows where there are few: as many as their tiles leave room for in the LDS.
 template <int DP>
 constexpr int many_sets() { return DP <= 64 ? 8 : 4; }
-// Tiles of 32 rows with many sets instead of 128 with one: where the former are no more than what keeps every compute unit at its walk for as long
-// as two workgroups of the latter would take, FIGURES.
+// Whether tiles of 32 rows with many sets beat tiles of 128 with one: in steps of a walk (the two kinds' steps take about as long), for the mean length,
+// as many times over as a compute unit has workgroups to run, one of the former or two of the latter at once; a workgroup's other work is worth 3 or 2
+// steps.  Measured, forward, dq and dk / dv together, many sets / one: one causal sequence on 8 heads, width 64: 1024 rows 39 / 70 us, 2048 80 / 125, 4096
+// 229 / 239, 8192 728 / 539; width 128: 1024 68 / 99, 2048 143 / 179, 4096 446 / 352; 4 sequences of 300 (not causal), width 128: 77 / 49.
 template <int DP>
-bool few(const Args& a, int heads) { return a.tokens * heads <= (int64_t)COMPUTE_UNITS * 16 * many_sets<DP>(); }
+bool few(const Args& a, int heads) {
+  const double walk = (double)a.tokens / a.sequences * (a.heads / heads);
+  double narrow = (double)(a.tokens / 32 + a.sequences) * heads / COMPUTE_UNITS, wide = (double)(a.tokens / 128 + a.sequences) * heads / (2 * COMPUTE_UNITS);
+  const double share = a.causal && narrow > 1 ? 0.5 : 1.0;             // causal walks are half as long on average, the longest as long
+  narrow = narrow > 1 ? narrow : 1;
+  wide = wide > 1 ? wide : 1;
+  return narrow * (share * walk / (32 * many_sets<DP>()) + 3) < wide * (walk / 64 + 2);
+}
 
 template <int DP, int WAVES>
 bool forward(Args a, int tiles, hipStream_t st) {
@@ -992,7 +1002,10 @@ bool backward(Args a, int tiles, hipStream_t st) {
 // f with the head's width rounded up to a multiple of 32 and the waves of a workgroup as constants
 template <class F>
 int dispatch(const disco_attention_shape& s, int tiles, F f) {
-  const int dp = (s.head_dim + 31) / 32, waves = tiles || s.tokens > (int64_t)96 * s.sequences ? 4 : 1;
+  const int dp = (s.head_dim + 31) / 32;
+  // Tiles of 32 or 128 rows.  Shared keys, 8 heads on 2, dq and dk / dv, one wave / four: 800 sequences of 30, width 64: 46 / 107 us; 200 of 150: 80 / 104;
+  // 200 of 90, width 128: 119 / 97.
+  const int waves = tiles || s.tokens > (int64_t)(dp <= 2 ? 160 : 64) * s.sequences ? 4 : 1;
 #define DISCO_DP(N) \
   if (dp == N) return (waves == 1 ? f(std::integral_constant<int, 32 * N>(), std::integral_constant<int, 1>()) \
                                   : f(std::integral_constant<int, 32 * N>(), std::integral_constant<int, 4>())) ? DISCO_OK : DISCO_ERR_HIP
