@@ -67,9 +67,9 @@ __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
   if (a.sequences <= 64) {
     const bool there = lane < a.sequences;
     const int first = there ? start(lane) : 0, mine = there ? start(lane + 1) - first : 0, tiles = mine > a.above ? (mine - 1) / T + 1 : 0;
-    auto later = [&](int k) { return wave_reduce(tiles >= k ? tiles - k + 1 : 0, [](int x, int y) { return x + y; }); };
+    auto later = [&](int k) { return __builtin_amdgcn_readfirstlane(wave_reduce(tiles >= k ? tiles - k + 1 : 0, [](int x, int y) { return x + y; })); };
     if (slot >= later(1)) return false;
-    int k = 1, over = wave_reduce(tiles, [](int x, int y) { return x > y ? x : y; }) + 1, before = 0;      // N(k) > slot >= N(over) = before
+    int k = 1, over = __builtin_amdgcn_readfirstlane(wave_reduce(tiles, [](int x, int y) { return x > y ? x : y; })) + 1, before = 0;      // N(k) > slot >= N(over) = before
     while (over - k > 1) {
       const int mid = (k + over) / 2, n = later(mid);
       if (n > slot) k = mid;
@@ -100,6 +100,10 @@ __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
     len = __builtin_amdgcn_readfirstlane(start(lo + 1)) - from;
     index = slot - (from / T + lo);
   }
+  // the same in every lane, and known to be
+  index = __builtin_amdgcn_readfirstlane(index);
+  from = __builtin_amdgcn_readfirstlane(from);
+  len = __builtin_amdgcn_readfirstlane(len);
   const int count = (len + T - 1) / T;
   t.first = from;
   t.len = len;
@@ -696,8 +700,8 @@ template <int WAVES>
 __device__ __forceinline__ bool short_sequence(const Args& a, int s, int64_t& first, int& len) {
   const int tokens = (int)a.tokens, x = a.starts[s], y = a.starts[s + 1];
   const int from = x < 0 ? 0 : x > tokens ? tokens : x, to = y < 0 ? 0 : y > tokens ? tokens : y;
-  first = from;
-  len = to - from;
+  first = __builtin_amdgcn_readfirstlane(from);
+  len = __builtin_amdgcn_readfirstlane(to - from);
   return len > 32 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) && len <= 32 * WAVES;
 }
 template <int DP>
@@ -920,10 +924,10 @@ void with_short(int tiles, F f) {
     else f(std::integral_constant<int, 8>());
   }
 }
-// The workgroups of a kernel that takes what is left, whole slots: few enough to end at once where nothing is (4.6 us; 16 times as many as the chip has
-// units: 7), enough to share out what is (1000 sequences of 1 to 300, forward: 40 us, with 2 times 52).
+// The workgroups of a kernel that takes what is left, whole slots: what the chip holds at once, as there is mostly nothing and they only end (1024 captions of
+// up to 77 tokens, forward and backward: 96 us a pass; with four times as many workgroups 102, for 40 us instead of 52 where 1000 sequences of 1 to 300 leave some).
 unsigned rest_grid(const Args& a, int heads) {
-  const int64_t slots = (8 * COMPUTE_UNITS + heads - 1) / heads;
+  const int64_t slots = (2 * COMPUTE_UNITS + heads - 1) / heads;
   return (unsigned)((slots < a.slots ? slots : a.slots) * heads);
 }
 bool launched() { return hipGetLastError() == hipSuccess; }
