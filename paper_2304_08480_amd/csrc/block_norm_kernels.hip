@@ -248,28 +248,32 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256, (waves_bwd<POST, PRE, NA
   const bool need_h = POST || a.gate != DISCO_GATE_NONE;
   for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.rows; r0 += (int64_t)gridDim.x * ROWS) {
     const bool there = r0 + own < a.rows;
-    const int64_t row = there ? r0 + own : a.rows - 1;
-    const float once = there ? 1.f : 0.f;
+    const int64_t row = r0 + own;
+    // a row that is not there is all zeros, and so is what it adds to the sums
     Raw ry = {}, rn = {}, rh = {}, rg = {}, rt = {};
-    if (a.dy) rt = load_raw(a.dy, row, d, col, a.x_bf16);
-    if (PRE) { ry = load_raw(a.y, row, d, col, a.x_bf16); rn = load_raw(a.dn, row, d, col, a.h_bf16); }
-    if (need_h) rh = load_raw(a.h, row, d, col, a.h_bf16);
-    if (a.gate == DISCO_GATE_ELEMENT) rg = load_raw(a.gate_values, row, d, col, a.h_bf16);
-    const float* st = a.stats + row * 4;
+    float m2 = 0.f, r2 = 0.f, m1 = 0.f, r1 = 0.f;
+    if (there) {
+      if (a.dy) rt = load_raw(a.dy, row, d, col, a.x_bf16);
+      if (PRE) { ry = load_raw(a.y, row, d, col, a.x_bf16); rn = load_raw(a.dn, row, d, col, a.h_bf16); }
+      if (need_h) rh = load_raw(a.h, row, d, col, a.h_bf16);
+      if (a.gate == DISCO_GATE_ELEMENT) rg = load_raw(a.gate_values, row, d, col, a.h_bf16);
+      const float* st = a.stats + row * 4;
+      if (PRE) { m1 = st[2]; r1 = st[3]; }
+      if (POST) { m2 = st[0]; r2 = st[1]; }
+    }
     float t[COLS];
     values<NARROW>(rt, a.x_bf16, t);
     if (PRE) {
       float y[COLS], dn[COLS], p[COLS], q[COLS];
       values<NARROW>(ry, a.x_bf16, y);
       values<NARROW>(rn, a.h_bf16, dn);
-      const float m1 = st[2], r1 = st[3];
 #pragma unroll
       for (int e = 0; e < COLS; ++e) {
         y[e] = (y[e] - m1) * r1;
         p[e] = dn[e] * w1[e];
         q[e] = p[e] * y[e];
-        sum[3][e] = fmaf(once * dn[e], y[e], sum[3][e]);
-        sum[4][e] = fmaf(once, dn[e], sum[4][e]);
+        sum[3][e] = fmaf(dn[e], y[e], sum[3][e]);
+        sum[4][e] += dn[e];
       }
       float s1 = sum8(p), s2 = sum8(q);
       total(s1, s2);
@@ -287,8 +291,6 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256, (waves_bwd<POST, PRE, NA
     float h[COLS];
     values<NARROW>(rh, a.h_bf16, h);
     if (a.gate == DISCO_GATE_ELEMENT) values<NARROW>(rg, a.h_bf16, g);
-    float m2 = 0.f, r2 = 1.f;
-    if (POST) { m2 = st[0]; r2 = st[1]; }
     float du[COLS], dg[COLS];
 #pragma unroll
     for (int e = 0; e < COLS; ++e) {
@@ -296,15 +298,15 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256, (waves_bwd<POST, PRE, NA
       const float u = POST ? fmaf(h[e], w2[e], b2[e]) : h[e];
       dg[e] = a.h_scale * t[e] * u;
       du[e] = a.h_scale * g[e] * t[e];
-      sum[0][e] = fmaf(once, dg[e], sum[0][e]);
+      sum[0][e] += dg[e];
     }
     if (there && a.dgate_rows) store(a.dgate_rows, row, d, col, a.h_bf16, dg);
     if (POST) {
       float p[COLS], q[COLS];
 #pragma unroll
       for (int e = 0; e < COLS; ++e) {
-        sum[1][e] = fmaf(once * du[e], h[e], sum[1][e]);
-        sum[2][e] = fmaf(once, du[e], sum[2][e]);
+        sum[1][e] = fmaf(du[e], h[e], sum[1][e]);
+        sum[2][e] += du[e];
         p[e] = du[e] * w2[e];
         q[e] = p[e] * h[e];
       }

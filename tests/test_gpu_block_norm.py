@@ -255,3 +255,28 @@ def test_captured_twice_and_on_two_streams():
     torch.cuda.synchronize()
     for n, want in zip((a, b), eager):
         assert all(torch.equal(want[k], x) for k, x in n.outputs().items())
+
+
+@pytest.mark.parametrize("rows,d", [(17, 100), (5, 500), (2049, 130)])
+def test_an_infinity_in_the_last_row_of_a_workgroup_that_has_rows_to_spare(rows, d):
+    """A workgroup's places behind the last row add nothing to the sums, whatever the last row holds: sums of one infinity are infinite, not NaN."""
+    n = Norm(rows, d, "layer", "none", "channel", "f32", "f32")
+    n.forward()
+    n.dev["dy"][rows - 1] = 1e30
+    n.shape.x_scale = 1e30                                      # dx = x_scale dy is infinite
+    n.backward()
+    want = n.outputs()
+    assert torch.isinf(want["dx"][rows - 1]).all() and all(torch.isfinite(want[k]).all() for k in ("dgate", "dw_post", "db_post"))
+    v = n.dev
+    dl.disco_block_norm_bwd(n.shape, v["dy"], v["dn"], v["h"], v["y"], v["gate"], v["w_post"], v["b_post"], v["w_pre"], v["stats"], v["dy"], v["dh"],
+                            v["dgate"], v["dw_post"], v["db_post"], v["dw_pre"], v["db_pre"], n.ws, n.need, torch.cuda.current_stream())
+    v["dx"] = v["dy"]
+    got = n.outputs()
+    assert all(torch.equal(got[k], want[k]) for k in got)
+    n = Norm(rows, d, "none", "layer", "none", "f32", "f32")
+    n.forward()
+    n.dev["dn"][rows - 1, 3] = float("inf")
+    n.backward()
+    got = n.outputs()
+    assert got["db_pre"][3] == float("inf") and torch.isfinite(got["db_pre"][[i for i in range(d) if i != 3]]).all()
+    assert torch.equal(torch.isnan(got["dw_pre"]), torch.zeros(d, dtype=torch.bool))
