@@ -299,9 +299,9 @@ DISCO_API int disco_logit_scale_bwd(const float* theta, float s_max, const float
  * q, k, v, o and the gradients are bf16 (dtype DISCO_BF16); lse is heads x tokens fp32, kept for the backward pass.  Scores, softmax and sums are
  * fp32, the softmax values and their gradients are rounded to bf16 before they are multiplied by v, dout, k and q.
  * Rows before the first and behind the last sequence are neither read nor written.  A NaN or infinity stays within its sequence; inside it, one can also
- * reach rows up to 31 away that the mask hides from it, as 0 times NaN.
+ * reach rows up to 63 away that the mask hides from it, as 0 times NaN.
  * All 16 bytes aligned, strides multiples of 8; head_dim a multiple of 8 up to 128 (else DISCO_ERR_UNSUPPORTED).  tokens < 2^31,
- * sequences <= 2^24, heads <= 2^16, (tokens / 32 + sequences) heads < 2^31, scale > 0, row strides in 1 .. 2^24, head strides
+ * sequences <= 2^24, heads <= 2^16, (tokens / 32 + 8 sequences) heads < 2^26, scale > 0, row strides in 1 .. 2^22, head strides
  * in 1 .. 2^40 (else DISCO_ERR_SHAPE).  Outputs overlap
  * nothing else (q, k, v may be views of one buffer, and so may dq, dk, dv).  Equal calls give equal bits.
  *

@@ -108,7 +108,7 @@ __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
   t.first = from;
   t.len = len;
   t.row = (KEYS && a.causal ? count - 1 - index : index) * T;
-  return index < count && len > a.above;
+  return index >= 0 && index < count && len > a.above;
 }
 
 // Whether any sequence is left to the kernels that follow those for short sequences: they are launched before that is known, as few workgroups, and
@@ -873,12 +873,12 @@ int check(const disco_attention_shape* s) {
   if (s->tokens <= 0 || s->tokens > 0x7fffffff || s->sequences <= 0 || s->sequences > 1 << 24 || s->heads <= 0 || s->kv_heads <= 0 ||
       s->heads > 1 << 16 || s->heads % s->kv_heads != 0 || s->head_dim <= 0 || !(s->scale > 0.f) || !isfinite(s->scale))
     return DISCO_ERR_SHAPE;
-  // what one launch of 32-row tiles has workgroups for
-  if ((s->tokens / 32 + s->sequences) * s->heads > 0x7fffffff) return DISCO_ERR_SHAPE;
+  // a launch has less than 2^32 threads: 64 for a tile of 32 rows, up to 512 for a sequence
+  if ((s->tokens / 32 + (int64_t)s->sequences * 8) * s->heads >= (int64_t)1 << 26) return DISCO_ERR_SHAPE;
   if (s->dtype != DISCO_BF16 || s->head_dim % 8 != 0 || s->head_dim > 128) return DISCO_ERR_UNSUPPORTED;
-  // the 64 rows of a tile are addressed with 32 bits
+  // the rows of a walked tile, 256 at most, are addressed with 32 bits
   for (int64_t v : {s->q_row, s->k_row, s->v_row, s->o_row}) {
-    if (v <= 0 || v > (int64_t)1 << 24) return DISCO_ERR_SHAPE;
+    if (v <= 0 || v > (int64_t)1 << 22) return DISCO_ERR_SHAPE;
     if (v % 8 != 0) return DISCO_ERR_UNSUPPORTED;
   }
   for (int64_t v : {s->q_head, s->k_head, s->v_head, s->o_head}) {
@@ -901,7 +901,6 @@ Args args_of(const disco_attention_shape& s, const int32_t* starts) {
 }
 
 constexpr int COMPUTE_UNITS = 256;
-
 
 // Tiles of 32 rows that the kernels for short sequences take, 0: none.  The lengths are on the device; the mean says what they may be.  Two and a half
 // times the mean where that is at most the widest: few sequences are longer, and a workgroup's idle waves cost the rest occupancy (500 sequences of

@@ -50,3 +50,15 @@ def test_workspace():
     assert _calls(_shape(), n=need - 1) == [dl.DISCO_ERR_WORKSPACE]
     with pytest.raises(dl.DiscoError, match="disco_attention_fwd"):
         dl.disco_attention_fwd(_shape(heads=0), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE)
+
+
+@pytest.mark.parametrize("kw", [dict(q_row=(1 << 22) + 8), dict(k_row=(1 << 22) + 8), dict(v_row=1 << 23), dict(o_row=1 << 24),
+                                dict(sequences=1 << 20), dict(tokens=1 << 28, sequences=1), dict(sequences=8192, heads=1 << 10, kv_heads=1 << 10)])
+def test_beyond_the_32_bits_of_a_tile_s_addresses_and_of_a_launch(kw):
+    assert set(_calls(_shape(**kw))) == {dl.DISCO_ERR_SHAPE}
+    assert dl.disco_attention_workspace_bytes(_shape(**kw)) == 0
+
+
+def test_the_largest_row_stride_and_launch():
+    assert dl.disco_attention_workspace_bytes(_shape(q_row=1 << 22, k_row=1 << 22, v_row=1 << 22, o_row=1 << 22)) > 0
+    assert dl.disco_attention_workspace_bytes(_shape(sequences=(1 << 20) - 1)) > 0

@@ -215,3 +215,51 @@ def test_long_sequences_on_few_and_many_heads(heads, kv_heads, dim, causal):
     a.forward()
     a.backward()
     assert all(torch.equal(one[n], x) for n, x in a.outputs().items())
+
+
+def test_the_largest_row_stride_with_tiles_of_many_rows():
+    # 700 rows, 8 MiB apart: the rows of a walked tile span 2 GiB
+    print("case attention largest row stride", flush=True)
+    a = Attention([650, 50], 2, 1, 64, True, seed=9, scale=0.3)
+    a.forward()
+    a.backward()
+    want = a.outputs()
+    room, grads = (torch.empty(700, 1 << 22, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for j, n in enumerate("qkvo"):
+        wide = [t[:, 1024 * j:1024 * j + getattr(a, n).shape[1] * 64].view(700, -1, 64) for t in (room, grads)]
+        if n == "o":
+            a.o = wide[0]
+            do = grads[:, 1 << 21:(1 << 21) + 128].view(700, 2, 64)
+            do.copy_(a.do)
+            a.do = do
+        else:
+            wide[0].copy_(getattr(a, n))
+            setattr(a, n, wide[0])
+            setattr(a, "d" + n, wide[1])
+        setattr(a.shape, n + "_row", 1 << 22)
+        setattr(a.shape, n + "_head", 64)
+    a.forward()
+    a.backward()
+    got = a.outputs()
+    assert all(torch.equal(got[k], want[k]) for k in got)
+
+
+@pytest.mark.parametrize("lengths,heads", [([300], 2), ([200, 200], 40), ([96] * 80, 2), ([30] * 300, 2)], ids=str)
+def test_how_far_a_masked_nan_reaches(lengths, heads):
+    # the last row of the last sequence: no other sequence sees it, nor a row more than 63 ahead of it, in any direction of the pass
+    a = Attention(lengths, heads, heads, 64, True, seed=5)
+    a.forward()
+    a.backward()
+    want = a.outputs()
+    for t in (a.q, a.k, a.v, a.do):
+        t[-1] = float("nan")
+    a.forward()
+    assert torch.equal(a.o[:a.T - 64].float().cpu(), want["o"][:a.T - 64])
+    assert torch.equal(a.lse[:, :a.T - 1].cpu(), want["lse"][:, :a.T - 1])
+    a.backward()
+    got = a.outputs()
+    first = a.T - lengths[-1]
+    for n in ("dq", "dk", "dv"):
+        assert torch.equal(got[n][:first], want[n][:first]), n
+    assert torch.equal(got["dq"][:a.T - 64], want["dq"][:a.T - 64])
+    assert torch.isnan(got["dk"][a.T - 1]).all() and torch.isnan(got["o"][a.T - 1]).all()
