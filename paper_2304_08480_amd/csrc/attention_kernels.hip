@@ -757,66 +757,77 @@ __global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void k_attention_fwd_
   if (there && half == 0) a.lse[head * a.tokens + seq + mine] = f.top * a.scale + __builtin_amdgcn_logf(f.total) * LN2;
 }
 
-// heads == kv_heads
-template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void k_attention_bwd_short(Args a) {
-  using S = Short<DP, WAVES>;
+// heads == kv_heads.  Six or eight tiles are two for each wave, the i-th and the i-th last (causal walks then add up to the same in every wave): with half
+// the waves two workgroups fit a compute unit, and one computes while the other reads its rows or writes gradients (128 x 197, 12 heads of 64: 114 us
+// for 137 with a wave for each tile; 300 causal sequences of 70 to 180, 8 heads: 82 for 80).
+template <int DP, int TILES>
+struct ShortBwd {
+  static constexpr int OWN = DP <= 64 && TILES >= 6 ? 2 : 1, WAVES = TILES / OWN;
+};
+template <int DP, int TILES>
+__global__ __launch_bounds__((64 * ShortBwd<DP, TILES>::WAVES), (DP <= 64 && TILES < 6 ? 3 : 2)) void k_attention_bwd_short(Args a) {
+  using S = Short<DP, TILES>;
+  constexpr int OWN = ShortBwd<DP, TILES>::OWN;
   __shared__ __attribute__((aligned(16))) char lds[2 * S::ALL];
   __shared__ __attribute__((aligned(16))) float row_lse[S::ROWS], row_delta[S::ROWS];
   const int head = blockIdx.x % a.heads;
   int64_t seq;
   int len;
-  if (!short_sequence<WAVES>(a, blockIdx.x / a.heads, seq, len)) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, mine = 32 * wave + (lane & 31);
-  const bool there = mine < len;
+  if (!short_sequence<TILES>(a, blockIdx.x / a.heads, seq, len)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
   const int tiles = (len + 31) / 32;
   const float c = a.scale * LOG2E;
-  Rows<DP> q, dout, k, v;
-  const float lse2 = there ? a.lse[head * a.tokens + seq + mine] * LOG2E : INFINITY;      // exp2(-inf) = 0
-  float delta = 0.f;
-  {
+  auto tile_of = [&](int i) { return i ? TILES - 1 - wave : wave; };
+  Rows<DP> q[OWN], dout[OWN];
+  float lse2[OWN], delta[OWN];
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) {
+    const int tile = tile_of(i), mine = 32 * tile + (lane & 31);
+    lse2[i] = mine < len ? a.lse[head * a.tokens + seq + mine] * LOG2E : INFINITY;      // exp2(-inf) = 0
+    delta[i] = 0.f;
     Stage<DP, 32, 64> sq, sk, sv, so, sd;
     sq.init(a.q_row, a.head_dim);
     sk.init(a.k_row, a.head_dim);
     sv.init(a.v_row, a.head_dim);
     so.init(a.o_row, a.head_dim);
     sd.init(a.o_row, a.head_dim);
-    const int64_t row = seq + 32 * wave;
-    const int rows = len - 32 * wave;
+    const int64_t row = seq + 32 * tile;
+    const int rows = len - 32 * tile;
     sq.fetch(a.q + row * a.q_row + head * a.q_head, a.q_row, rows, a.head_dim);
     sd.fetch(a.dout + row * a.o_row + head * a.o_head, a.o_row, rows, a.head_dim);
     so.fetch(a.o + row * a.o_row + head * a.o_head, a.o_row, rows, a.head_dim);
     sk.fetch(a.k + row * a.k_row + head * a.k_head, a.k_row, rows, a.head_dim);
     sv.fetch(a.v + row * a.v_row + head * a.v_head, a.v_row, rows, a.head_dim);
-    char* own = lds + wave * S::SUB;
+    char* own = lds + tile * S::SUB;
     Rows<DP> o;
     sq.put(own);
     sd.put(own + S::ALL);
-    take_rows<DP>(own, q);
-    take_rows<DP>(own + S::ALL, dout);
+    take_rows<DP>(own, q[i]);
+    take_rows<DP>(own + S::ALL, dout[i]);
     so.put(own);
     take_rows<DP>(own, o);
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) delta = fmaf((float)o.f[s][e], (float)dout.f[s][e], delta);
-    delta += other_half(delta);
+      for (int e = 0; e < 8; ++e) delta[i] = fmaf((float)o.f[s][e], (float)dout[i].f[s][e], delta[i]);
+    delta[i] += other_half(delta[i]);
     sk.put(own);
     sv.put(own + S::ALL);
-    take_rows<DP>(own, k);
-    take_rows<DP>(own + S::ALL, v);
   }
   __syncthreads();
-  {
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) {
+    const int tile = tile_of(i), mine = 32 * tile + (lane & 31);
+    if (tile >= tiles) break;
     f32x16 acc[DP / 32];
 #pragma unroll
     for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
-    const int last = a.causal && there ? mine : len - 1, end = a.causal ? wave + 1 : tiles;
+    const int last = a.causal && mine < len ? mine : len - 1, end = a.causal ? tile + 1 : tiles;
     for (int t = 0; t < end; ++t) {
       const char* now = lds + t * S::SUB;
       f32x16 s[2];                                                  // scores, and dP
-      products<DP, 2, S::ALL>(s, now, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
-      if ((a.causal && t == wave) || 32 * t + 32 > len) {
+      products<DP, 2, S::ALL>(s, now, [&](int n, int p, int) { return n ? dout[i].f[p] : q[i].f[p]; });
+      if ((a.causal && t == tile) || 32 * t + 32 > len) {
         int most = last - 32 * t - 4 * half;
         asm volatile("" : "+v"(most));
 #pragma unroll
@@ -824,48 +835,63 @@ __global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void k_attention_bwd_
           if (walked(r, 0) > most) s[0][r] = -INFINITY;
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2)) * (s[1][r] - delta);
+      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2[i])) * (s[1][r] - delta[i]);
       accumulate<DP, 1, 0>({&acc}, now, {rounded(s[0])});
     }
-    store_row<DP>(a.dq + (seq + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, there);
+    store_row<DP>(a.dq + (seq + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, mine < len);
+  }
+  Rows<DP> k[OWN], v[OWN];
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) {
+    take_rows<DP>(lds + tile_of(i) * S::SUB, k[i]);
+    take_rows<DP>(lds + S::ALL + tile_of(i) * S::SUB, v[i]);
   }
   __syncthreads();
-  put_rows<DP>(lds + wave * S::SUB, q);
-  put_rows<DP>(lds + S::ALL + wave * S::SUB, dout);
-  if (half == 0) {
-    row_lse[mine] = lse2;
-    row_delta[mine] = delta;
-  }
-  __syncthreads();
-  f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
-  for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
-  for (int t = a.causal ? wave : 0; t < tiles; ++t) {
-    const char* now = lds + t * S::SUB;
-    f32x16 s[2];
-    products<DP, 2, S::ALL>(s, now, [&](int n, int i, int) { return n ? v.f[i] : k.f[i]; });
-    if (a.causal && t == wave) {
-      int least = mine - 32 * t - 4 * half;
-      asm volatile("" : "+v"(least));
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (walked(r, 0) < least) s[0][r] = -INFINITY;
+  for (int i = 0; i < OWN; ++i) {
+    const int tile = tile_of(i), mine = 32 * tile + (lane & 31);
+    put_rows<DP>(lds + tile * S::SUB, q[i]);
+    put_rows<DP>(lds + S::ALL + tile * S::SUB, dout[i]);
+    if (half == 0) {
+      row_lse[mine] = lse2[i];
+      row_delta[mine] = delta[i];
     }
-    const float *lse = row_lse + 32 * t + 4 * half, *del = row_delta + 32 * t + 4 * half;
+  }
+  __syncthreads();
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4 l = *reinterpret_cast<const f32x4*>(lse + 8 * g), d = *reinterpret_cast<const f32x4*>(del + 8 * g);
+  for (int i = 0; i < OWN; ++i) {
+    const int tile = tile_of(i), mine = 32 * tile + (lane & 31);
+    if (tile >= tiles) break;
+    f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = 4 * g + e;
-        s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
-        s[1][r] = s[0][r] * (s[1][r] - d[e]);
+    for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
+    for (int t = a.causal ? tile : 0; t < tiles; ++t) {
+      const char* now = lds + t * S::SUB;
+      f32x16 s[2];
+      products<DP, 2, S::ALL>(s, now, [&](int n, int p, int) { return n ? v[i].f[p] : k[i].f[p]; });
+      if (a.causal && t == tile) {
+        int least = mine - 32 * t - 4 * half;
+        asm volatile("" : "+v"(least));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (walked(r, 0) < least) s[0][r] = -INFINITY;
       }
+      const float *lse = row_lse + 32 * t + 4 * half, *del = row_delta + 32 * t + 4 * half;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 l = *reinterpret_cast<const f32x4*>(lse + 8 * g), d = *reinterpret_cast<const f32x4*>(del + 8 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * g + e;
+          s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
+          s[1][r] = s[0][r] * (s[1][r] - d[e]);
+        }
+      }
+      accumulate<DP, 2, S::ALL>({&dk, &dv}, now, {rounded(s[1]), rounded(s[0])});
     }
-    accumulate<DP, 2, S::ALL>({&dk, &dv}, now, {rounded(s[1]), rounded(s[0])});
+    store_row<DP>(a.dk + (seq + mine) * a.k_row + head * a.k_head, dk, a.scale, a.head_dim, mine < len);
+    store_row<DP>(a.dv + (seq + mine) * a.v_row + head * a.v_head, dv, 1.f, a.head_dim, mine < len);
   }
-  store_row<DP>(a.dk + (seq + mine) * a.k_row + head * a.k_head, dk, a.scale, a.head_dim, there);
-  store_row<DP>(a.dv + (seq + mine) * a.v_row + head * a.v_head, dv, 1.f, a.head_dim, there);
 }
 
 int check(const disco_attention_shape* s) {
@@ -994,7 +1020,7 @@ bool backward(Args a, int tiles, hipStream_t st) {
     return launched();
   }
   a.above = 32 * tiles;
-  with_short<DP>(tiles, [&](auto w) { k_attention_bwd_short<DP, w()><<<(unsigned)(a.sequences * a.heads), 64 * w(), 0, st>>>(a); });
+  with_short<DP>(tiles, [&](auto w) { k_attention_bwd_short<DP, w()><<<(unsigned)(a.sequences * a.heads), 64 * ShortBwd<DP, w()>::WAVES, 0, st>>>(a); });
   if (!launched() || a.tokens <= a.above) return launched();
   k_attention_bwd_q_rest<DP><<<rest_grid(a, a.heads), 256, 0, st>>>(a);
   if (!launched()) return false;
