@@ -928,15 +928,21 @@ Args args_of(const disco_attention_shape& s, const int32_t* starts) {
 
 constexpr int COMPUTE_UNITS = 256;
 
-// Tiles of 32 rows that the kernels for short sequences take, 0: none.  The lengths are on the device; the mean says what they may be.  Two and a half
-// times the mean where that is at most the widest: few sequences are longer, and a workgroup's idle waves cost the rest occupancy (500 sequences of
-// 60 tokens, 8 heads of 64, forward and backward: 81 us with 4 tiles, 98 with 8, 101 without these kernels).  The widest up to 4/5 of it: sequences of
-// one length, as images have (128 x 197, 12 heads: 181 against 220 without).
+// Tiles of 32 rows that the kernels for short sequences take, 0: none.  The lengths are on the device; the mean says what they may be.  2.8 times
+// the mean where that is at most the widest: few sequences are longer (of lengths spread evenly over the decades from 4 to 77 the longest is 3.1 times the
+// mean), and tiles that are not there cost the rest occupancy.  Forward and backward, 8 heads of 64: 500 sequences of 44, 63 us with 4 tiles, 79 with 6, 84
+// without these kernels; 400 of 8 to 120, 59, 72 and 74; 150 of 4 to 77, 23 with 3 tiles, 51 with 2, which leave some.  The widest up to 4/5 of it:
+// sequences of one length, as images have (128 x 197, 12 heads: 160 against 220 without).
+//
+// None for few and short sequences of narrow heads, either kind of kernel is done at once and these are five launches for three (150 of 4 to 77
+// on 8 heads, with and without: 32 and 25 us where the host is the slower, 23 and 23 in a graph; 1000 of them 76 and 108); of up to 96 rows in all these leave
+// nothing and are two (2 of 40: 10 and 14).
 int short_tiles(const disco_attention_shape& s, bool backward) {
   if ((backward && s.heads != s.kv_heads) || s.sequences > 8192) return 0;
   const int widest = s.head_dim <= 64 ? 8 : 4;
+  if (s.head_dim <= 64 && s.tokens <= (int64_t)s.sequences * 64 && s.tokens > 96 && (int64_t)s.sequences * s.heads <= 5 * COMPUTE_UNITS) return 0;
   for (int w : {2, 3, 4, 6})
-    if (w <= widest && s.tokens * 5 <= (int64_t)s.sequences * (32 * w * 2)) return w;
+    if (w <= widest && s.tokens * 28 <= (int64_t)s.sequences * (32 * w * 10)) return w;
   return s.tokens * 5 <= (int64_t)s.sequences * (32 * widest * 4) ? widest : 0;
 }
 template <int DP, class F>

@@ -263,3 +263,17 @@ def test_how_far_a_masked_nan_reaches(lengths, heads):
         assert torch.equal(got[n][:first], want[n][:first]), n
     assert torch.equal(got["dq"][:a.T - 64], want["dq"][:a.T - 64])
     assert torch.isnan(got["dk"][a.T - 1]).all() and torch.isnan(got["o"][a.T - 1]).all()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dim", [32, 64])
+@pytest.mark.parametrize("typical,longer", [(18, 64), (18, 65), (30, 97), (40, 128), (40, 300), (60, 193), (62, 257)])
+def test_thousands_of_short_sequences_and_heads(typical, longer, dim, causal):
+    # as above, where there are more than a few of them
+    print("case attention many", typical, longer, dim, causal, flush=True)
+    g = torch.Generator().manual_seed(typical + longer)
+    lengths = torch.randint(0, 2 * typical + 1, (330,), generator=g).tolist()
+    a = Attention([longer] + lengths[:160] + [longer, 0, 32, 33] + lengths[160:] + [longer + 1], 4, 4, dim, causal, seed=dim, behind=3)
+    a.forward()
+    a.backward()
+    a.check()
