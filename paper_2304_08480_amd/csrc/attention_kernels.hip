@@ -42,7 +42,6 @@ struct Args {
   const __bf16 *q, *k, *v, *o, *dout;
   __bf16 *out, *dq, *dk, *dv;
   float *lse, *delta;
-  int32_t slots;
   int32_t above;                // sequences of up to this many rows are another kernel's
 };
 
@@ -66,7 +65,7 @@ __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
   int from, len, index;
   if (a.sequences <= 64) {
     const bool there = lane < a.sequences;
-    const int first = there ? start(lane) : 0, mine = there ? start(lane + 1) - first : 0, tiles = mine > a.above ? (mine - 1) / T + 1 : 0;
+    const int first = there ? start(lane) : 0, mine = there ? start(lane + 1) - first : 0, tiles = mine > 0 ? (mine - 1) / T + 1 : 0;
     auto later = [&](int k) { return __builtin_amdgcn_readfirstlane(wave_reduce(tiles >= k ? tiles - k + 1 : 0, [](int x, int y) { return x + y; })); };
     if (slot >= later(1)) return false;
     int k = 1, over = __builtin_amdgcn_readfirstlane(wave_reduce(tiles, [](int x, int y) { return x > y ? x : y; })) + 1, before = 0;      // N(k) > slot >= N(over) = before
@@ -108,15 +107,39 @@ __device__ __forceinline__ bool find_tile(const Args& a, int slot, Tile& t) {
   t.first = from;
   t.len = len;
   t.row = (KEYS && a.causal ? count - 1 - index : index) * T;
-  return index >= 0 && index < count && len > a.above;
+  return index >= 0 && index < count;
 }
 
-// Whether any sequence is left to the kernels that follow those for short sequences: they are launched before that is known, as few workgroups, and
-// mostly end here.
-__device__ __forceinline__ bool any_rest(const Args& a) {
+// What is left to the kernels that follow those for short sequences, f(tile) for the tiles of T rows of all longer ones dealt to `stride` groups of
+// workgroups in turn.  They are launched before it is known that there are any, as few workgroups, and mostly end after one look at the lengths (4.8 us).  300 sequences of 10 to 197, of which a dozen are left, forward and backward: 100 us; with the search of
+// find_tile for every tile 113.
+template <int T, bool KEYS, class F>
+__device__ __forceinline__ void each_rest(const Args& a, int group, int stride, F f) {
+  const int lane = threadIdx.x & 63, tokens = (int)a.tokens;
+  auto start = [&](int s) { const int v = a.starts[s]; return v < 0 ? 0 : v > tokens ? tokens : v; };
   bool any = false;
-  for (int s = threadIdx.x; s < a.sequences; s += blockDim.x) any |= a.starts[s + 1] - a.starts[s] > a.above;
-  return __syncthreads_or(any);
+  for (int s = threadIdx.x; s < a.sequences; s += blockDim.x) any |= start(s + 1) - start(s) > a.above;
+  if (!__syncthreads_or(any)) return;
+  int next = group;                                                  // the group's next tile, counted from the first of the sequence at hand
+#pragma nounroll
+  for (int base = 0; base < a.sequences; base += 64) {
+    const bool there = base + lane < a.sequences;
+    const int first = there ? start(base + lane) : 0, len = there ? start(base + lane + 1) - first : 0;
+#pragma nounroll
+    for (uint64_t longer = __ballot(len > a.above); longer; longer &= longer - 1) {
+      const int s = __ffsll((unsigned long long)longer) - 1;
+      Tile t;
+      t.first = __builtin_amdgcn_readlane(first, s);
+      t.len = __builtin_amdgcn_readlane(len, s);
+      const int count = (t.len - 1) / T + 1;
+#pragma nounroll
+      for (; next < count; next += stride) {
+        t.row = (KEYS && a.causal ? count - 1 - next : next) * T;
+        f(t);
+      }
+      next -= count;
+    }
+  }
 }
 
 // A walked tile in the LDS: rows of DP elements, padded to a power of two of bytes, 16-byte pieces XOR-ed with bits of the row so that
@@ -467,11 +490,7 @@ __global__ __launch_bounds__(64 * WAVES * SETS, 2) void k_attention_fwd(Args a) 
 template <int DP>
 __global__ __launch_bounds__(256, 2) void k_attention_fwd_rest(Args a) {
   __shared__ __attribute__((aligned(16))) char lds[Shape<DP, 4, 1>::LDS];
-  if (!any_rest(a)) return;
-  Tile t;
-#pragma nounroll
-  for (int slot = blockIdx.x / a.heads; slot < a.slots; slot += gridDim.x / a.heads)
-    if (find_tile<128, false>(a, slot, t)) forward_tile<DP, 4, 1>(a, t, blockIdx.x % a.heads, lds);
+  each_rest<128, false>(a, blockIdx.x / a.heads, gridDim.x / a.heads, [&](const Tile& t) { forward_tile<DP, 4, 1>(a, t, blockIdx.x % a.heads, lds); });
 }
 
 // dq, and delta = <do, o> of every row for the kernel of dk and dv, which runs after this one.
@@ -559,11 +578,7 @@ __global__ __launch_bounds__(64 * WAVES * SETS, 2) void k_attention_bwd_q(Args a
 template <int DP>
 __global__ __launch_bounds__(256, 2) void k_attention_bwd_q_rest(Args a) {
   __shared__ __attribute__((aligned(16))) char lds[Shape<DP, 4, 1>::LDS];
-  if (!any_rest(a)) return;
-  Tile t;
-#pragma nounroll
-  for (int slot = blockIdx.x / a.heads; slot < a.slots; slot += gridDim.x / a.heads)
-    if (find_tile<128, false>(a, slot, t)) queries_tile<DP, 4, 1>(a, t, blockIdx.x % a.heads, lds);
+  each_rest<128, false>(a, blockIdx.x / a.heads, gridDim.x / a.heads, [&](const Tile& t) { queries_tile<DP, 4, 1>(a, t, blockIdx.x % a.heads, lds); });
 }
 
 // dk and dv: 32 keys a wave; the queries of all heads that share the keys are walked, head by head, 32 rows a step for each set.
@@ -681,11 +696,7 @@ __global__ __launch_bounds__(64 * WAVES * SETS, 2) void k_attention_bwd_kv(Args 
 template <int DP>
 __global__ __launch_bounds__(256, 2) void k_attention_bwd_kv_rest(Args a) {
   __shared__ __attribute__((aligned(16))) char lds[Keys<DP, 4, 1>::ALL];
-  if (!any_rest(a)) return;
-  Tile t;
-#pragma nounroll
-  for (int slot = blockIdx.x / a.kv_heads; slot < a.slots; slot += gridDim.x / a.kv_heads)
-    if (find_tile<128, true>(a, slot, t)) keys_tile<DP, 4, 1>(a, t, blockIdx.x % a.kv_heads, lds);
+  each_rest<128, true>(a, blockIdx.x / a.kv_heads, gridDim.x / a.kv_heads, [&](const Tile& t) { keys_tile<DP, 4, 1>(a, t, blockIdx.x % a.kv_heads, lds); });
 }
 
 // ---- Short sequences: a workgroup has all of one, WAVES tiles of 32 rows at most, for one head.  Every row is read from memory once and kept by its
@@ -956,10 +967,10 @@ void with_short(int tiles, F f) {
   }
 }
 // The workgroups of a kernel that takes what is left, whole slots: what the chip holds at once, as there is mostly nothing and they only end (1024 captions of
-// up to 77 tokens, forward and backward: 96 us a pass; with four times as many workgroups 102, for 40 us instead of 52 where 1000 sequences of 1 to 300 leave some).
+// up to 77 tokens, forward and backward: 96 us a pass; with four times as many workgroups 102).
 unsigned rest_grid(const Args& a, int heads) {
-  const int64_t slots = (2 * COMPUTE_UNITS + heads - 1) / heads;
-  return (unsigned)((slots < a.slots ? slots : a.slots) * heads);
+  const int64_t groups = (2 * COMPUTE_UNITS + heads - 1) / heads, tiles = a.tokens / 128 + a.sequences;
+  return (unsigned)((groups < tiles ? groups : tiles) * heads);
 }
 bool launched() { return hipGetLastError() == hipSuccess; }
 
@@ -984,13 +995,13 @@ template <int DP, int WAVES>
 bool forward(Args a, int tiles, hipStream_t st) {
   if (!tiles && WAVES > 1 && few<DP>(a, a.heads)) {
     constexpr int SETS = many_sets<DP>();
-    a.slots = (int)(a.tokens / 32) + a.sequences;
-    k_attention_fwd<DP, 1, SETS><<<(unsigned)(a.slots * a.heads), 64 * SETS, 0, st>>>(a);
+    const int64_t slots = a.tokens / 32 + a.sequences;
+    k_attention_fwd<DP, 1, SETS><<<(unsigned)(slots * a.heads), 64 * SETS, 0, st>>>(a);
     return launched();
   }
-  a.slots = (int)(a.tokens / (32 * WAVES)) + a.sequences;
   if (!tiles) {
-    k_attention_fwd<DP, WAVES, 1><<<(unsigned)(a.slots * a.heads), 64 * WAVES, 0, st>>>(a);
+    const int64_t slots = a.tokens / (32 * WAVES) + a.sequences;
+    k_attention_fwd<DP, WAVES, 1><<<(unsigned)(slots * a.heads), 64 * WAVES, 0, st>>>(a);
     return launched();
   }
   a.above = 32 * tiles;
@@ -1002,11 +1013,9 @@ bool forward(Args a, int tiles, hipStream_t st) {
 template <int DP, int WAVES>
 bool backward(Args a, int tiles, hipStream_t st) {
   constexpr int SETS = many_sets<DP>();
-  a.slots = (int)(a.tokens / (32 * WAVES)) + a.sequences;
   if (!tiles) {
-    const int wide = a.slots, narrow = (int)(a.tokens / 32) + a.sequences;
+    const int64_t wide = a.tokens / (32 * WAVES) + a.sequences, narrow = a.tokens / 32 + a.sequences;
     if (WAVES > 1 && few<DP>(a, a.heads)) {
-      a.slots = narrow;
       k_attention_bwd_q<DP, 1, SETS><<<(unsigned)(narrow * a.heads), 64 * SETS, 0, st>>>(a);
     } else {
       k_attention_bwd_q<DP, WAVES, 1><<<(unsigned)(wide * a.heads), 64 * WAVES, 0, st>>>(a);
@@ -1016,10 +1025,8 @@ bool backward(Args a, int tiles, hipStream_t st) {
     // 928 with one set; on 16 of keys, two workgroups of one set a unit, 640 against 585.
     const int64_t work = a.tokens / (32 * WAVES) * a.kv_heads / (a.causal ? 2 : 1);      // workgroups that have some, nearly
     if (WAVES > 1 && few<DP>(a, a.kv_heads)) {
-      a.slots = narrow;
       k_attention_bwd_kv<DP, 1, SETS><<<(unsigned)(narrow * a.kv_heads), 64 * SETS, 0, st>>>(a);
     } else {
-      a.slots = wide;
       if (WAVES == 1 || work > COMPUTE_UNITS) k_attention_bwd_kv<DP, WAVES, 1><<<(unsigned)(wide * a.kv_heads), 64 * WAVES, 0, st>>>(a);
       else k_attention_bwd_kv<DP, WAVES, WAVES == 1 ? 1 : 2><<<(unsigned)(wide * a.kv_heads), 128 * WAVES, 0, st>>>(a);
     }
