@@ -955,13 +955,14 @@ constexpr int COMPUTE_UNITS = 256;
 // without these kernels; 400 of 8 to 120, 59, 72 and 74; 150 of 4 to 77, 23 with 3 tiles, 51 with 2, which leave some.  The widest up to 4/5 of it:
 // sequences of one length, as images have (128 x 197, 12 heads: 160 against 220 without).
 //
-// None for few and short sequences of narrow heads, either kind of kernel is done at once and these are five launches for three (150 of 4 to 77
-// on 8 heads, with and without: 32 and 25 us where the host is the slower, 23 and 23 in a graph; 1000 of them 76 and 108); of up to 96 rows in all these leave
-// nothing and are two (2 of 40: 10 and 14).
+// None for few sequences of narrow heads that are short or, as causal ones mostly are, of different lengths: these kernels are five launches for three, and what
+// they leave then takes longest.  Forward and backward, with them and without: 150 of 4 to 77 on 8 heads, 32 and 25 us where the host is the slower, 23 and
+// 23 in a graph; 1000 of them 76 and 108; 40 of 1 to 1024 on 16 heads 181 and 111; 100 of 20 to 400 on 8 heads 95 and 82; but 12 images of 197 on 12 heads 37 and
+// 50.  Batches of up to 96 rows leave nothing and are two launches (2 of 40: 10 and 14).
 int short_tiles(const disco_attention_shape& s, bool backward) {
   if ((backward && s.heads != s.kv_heads) || s.sequences > 8192) return 0;
   const int widest = s.head_dim <= 64 ? 8 : 4;
-  if (s.head_dim <= 64 && s.tokens <= (int64_t)s.sequences * 64 && s.tokens > 96 && (int64_t)s.sequences * s.heads <= 5 * COMPUTE_UNITS) return 0;
+  if (s.head_dim <= 64 && (s.causal || s.tokens <= (int64_t)s.sequences * 64) && s.tokens > 96 && (int64_t)s.sequences * s.heads <= 5 * COMPUTE_UNITS) return 0;
   for (int w : {2, 3, 4, 6})
     if (w <= widest && s.tokens * 28 <= (int64_t)s.sequences * (32 * w * 10)) return w;
   return s.tokens * 5 <= (int64_t)s.sequences * (32 * widest * 4) ? widest : 0;
@@ -1001,6 +1002,12 @@ bool few(const Args& a, int heads) {
   return narrow * (share * walk / (32 * many_sets<DP>()) + 3) < wide * (walk / 64 + 2);
 }
 
+// Two sets of waves for tiles of 128 rows, where there are at most 3 halves (causal, with half the work: 3) of them for a compute unit: dk and dv of one sequence of 8192, causal,
+// head width 128, 16 heads on 8 of keys: 630 us against 928 with one set; on 16 of keys, two workgroups of one set a unit, 640 against 585.  Forward, 12 causal
+// sequences of 1 to 2048, 16 heads of 128: 43 against 52, 24 of them 143 against 112; 16 of 1 to 4096, 8 heads of 64: 57 against 74.
+template <int WAVES>
+bool two_sets(const Args& a, int heads) { return WAVES > 1 && a.tokens / (32 * WAVES) * heads / (a.causal ? 2 : 1) <= COMPUTE_UNITS * 3 / 2; }
+
 template <int DP, int WAVES>
 bool forward(Args a, int tiles, hipStream_t st) {
   if (!tiles && WAVES > 1 && few<DP>(a, a.heads)) {
@@ -1011,7 +1018,8 @@ bool forward(Args a, int tiles, hipStream_t st) {
   }
   if (!tiles) {
     const int64_t slots = a.tokens / (32 * WAVES) + a.sequences;
-    k_attention_fwd<DP, WAVES, 1><<<(unsigned)(slots * a.heads), 64 * WAVES, 0, st>>>(a);
+    if (two_sets<WAVES>(a, a.heads)) k_attention_fwd<DP, WAVES, WAVES == 1 ? 1 : 2><<<(unsigned)(slots * a.heads), 128 * WAVES, 0, st>>>(a);
+    else k_attention_fwd<DP, WAVES, 1><<<(unsigned)(slots * a.heads), 64 * WAVES, 0, st>>>(a);
     return launched();
   }
   a.above = 32 * tiles;
@@ -1027,18 +1035,17 @@ bool backward(Args a, int tiles, hipStream_t st) {
     const int64_t wide = a.tokens / (32 * WAVES) + a.sequences, narrow = a.tokens / 32 + a.sequences;
     if (WAVES > 1 && few<DP>(a, a.heads)) {
       k_attention_bwd_q<DP, 1, SETS><<<(unsigned)(narrow * a.heads), 64 * SETS, 0, st>>>(a);
+    } else if (two_sets<WAVES>(a, a.heads)) {
+      k_attention_bwd_q<DP, WAVES, WAVES == 1 ? 1 : 2><<<(unsigned)(wide * a.heads), 128 * WAVES, 0, st>>>(a);
     } else {
       k_attention_bwd_q<DP, WAVES, 1><<<(unsigned)(wide * a.heads), 64 * WAVES, 0, st>>>(a);
     }
     if (!launched()) return false;
-    // Two sets where the key tiles are no more than the compute units: one sequence of 8192, causal, head width 128, 16 heads on 8 of keys: 630 us against
-    // 928 with one set; on 16 of keys, two workgroups of one set a unit, 640 against 585.
-    const int64_t work = a.tokens / (32 * WAVES) * a.kv_heads / (a.causal ? 2 : 1);      // workgroups that have some, nearly
     if (WAVES > 1 && few<DP>(a, a.kv_heads)) {
       k_attention_bwd_kv<DP, 1, SETS><<<(unsigned)(narrow * a.kv_heads), 64 * SETS, 0, st>>>(a);
     } else {
-      if (WAVES == 1 || work > COMPUTE_UNITS) k_attention_bwd_kv<DP, WAVES, 1><<<(unsigned)(wide * a.kv_heads), 64 * WAVES, 0, st>>>(a);
-      else k_attention_bwd_kv<DP, WAVES, WAVES == 1 ? 1 : 2><<<(unsigned)(wide * a.kv_heads), 128 * WAVES, 0, st>>>(a);
+      if (two_sets<WAVES>(a, a.kv_heads)) k_attention_bwd_kv<DP, WAVES, WAVES == 1 ? 1 : 2><<<(unsigned)(wide * a.kv_heads), 128 * WAVES, 0, st>>>(a);
+      else k_attention_bwd_kv<DP, WAVES, 1><<<(unsigned)(wide * a.kv_heads), 64 * WAVES, 0, st>>>(a);
     }
     return launched();
   }

@@ -277,3 +277,13 @@ def test_thousands_of_short_sequences_and_heads(typical, longer, dim, causal):
     a.forward()
     a.backward()
     a.check()
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,causal,lengths", [(8, 8, 64, False, [695, 1063, 2000]), (8, 4, 128, True, [100, 923, 0, 2000, 1083, 1683]),
+                                                               (6, 2, 96, True, [1500, 31, 1601, 1]), (8, 8, 64, True, [2845, 1, 710, 128, 129])])
+def test_tiles_with_two_sets_of_waves(heads, kv_heads, dim, causal, lengths):
+    print("case attention two sets", heads, kv_heads, dim, causal, lengths, flush=True)
+    a = Attention(lengths, heads, kv_heads, dim, causal, seed=dim, behind=5)
+    a.forward()
+    a.backward()
+    a.check()
