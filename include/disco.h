@@ -358,7 +358,7 @@ DISCO_API int disco_block_norm_bwd(const disco_block_norm_shape* shape, const vo
 
 /*
  * The global norm of a step's gradients, and clipping by it.  A list of `count` tensors is four host arrays that are read during the call: device
- * pointers, numbers of elements (>= 0, a pointer may be NULL where it is 0), types (disco_dtype; gradients of different types may be mixed).
+ * pointers, numbers of elements (0 .. 2^40, less than 2^43 in all; a pointer may be NULL where it is 0), types (disco_dtype; gradients of different types may be mixed).
  *
  * disco_grad_norm: *norm = sqrt(sum of all squares), or with accumulate sqrt(*norm^2 + that sum), for lists that are taken in parts.  Squares are summed
  * in fp64 in a fixed order: no gradient that fp32 holds overflows or underflows, equal calls give equal bits.

@@ -193,7 +193,7 @@ int check(const void* const* src, void* const* dst, const int64_t* elements, con
     if ((reinterpret_cast<uintptr_t>(src[i]) | (writes ? reinterpret_cast<uintptr_t>(dst[i]) : 0)) & mask) return DISCO_ERR_UNSUPPORTED;
     all += elements[i] / PIECE + 1;
   }
-  return all <= 0x7fffffff ? DISCO_OK : DISCO_ERR_SHAPE;       // pieces are counted in 32 bits
+  return all <= 0x7fffffff - BLOCKS ? DISCO_OK : DISCO_ERR_SHAPE;       // a workgroup counts pieces in 32 bits, up to its first that is not there
 }
 
 // f(table) for every TABLE tensors that have elements, from the list's first or from its last

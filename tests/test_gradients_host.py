@@ -56,3 +56,10 @@ def test_lists_of_tensors():
     assert dl.disco_grad_norm([a.half()], FAKE, FAKE, 1 << 20, check=False) == dl.DISCO_ERR_UNSUPPORTED
     with pytest.raises(dl.DiscoError, match="disco_grad_clip"):
         dl.disco_grad_clip([a.half()], [a.half()], 1.0, None, FAKE, FAKE, 1 << 20)
+
+
+def test_more_pieces_than_a_workgroup_counts():
+    # pieces of 8192 elements: 2^31 - 1 - 1000 of them, and past them the step of 2048 workgroups
+    rest = ((1 << 31) - 1 - 1000 - 15 * ((1 << 27) + 1) - 1) * 8192
+    assert rest < 1 << 40
+    assert _calls(_list(16, elements=[1 << 40] * 15 + [rest]), count=16) == {dl.DISCO_ERR_SHAPE}
