@@ -12,9 +12,9 @@
 // Two kernels for the backward pass instead of one: each gradient is summed by one wave in a fixed order, in registers, with neither
 // atomics nor fp32 copies of dq, for 7 products instead of 5.
 //
-// Long sequences are bound by the SIMDs' issue: forward, matrix instructions take 40 % of the time and vector instructions 42 %, and with two
+// Long sequences are bound by the SIMDs' issue: forward, matrix instructions take 44 % of the time and vector instructions 45 %, and with two
 // waves a SIMD, which is what the registers allow, they overlap in part; the LDS has no conflicts.  One causal sequence of 8192, 16
-// heads of 128 on 8: forward 316 us (870 TFLOP/s of the products below the diagonal), dq 416 (990), dk and dv 630 (870); a large product by the vendor's
+// heads of 128 on 8: forward 302 us (910 TFLOP/s of the products below the diagonal), dq 411 (1000), dk and dv 601 (915); a large product by the vendor's
 // library reaches 1150 on the same card.  Short ones are bound by memory, at the rate of a copy but for the launches.
 //
 // Scores, statistics and sums are fp32.  P and dS are rounded to bf16 (by at most 2^-8 of each value) for the matrix instruction; the sum of P that
@@ -255,6 +255,12 @@ __device__ __forceinline__ void products(f32x16 (&c)[N], const char* lds, B b) {
   }
   interleave<AHEAD_P, 1, DP / 16 * N, DP / 16 * N>();
 }
+// A wave in its matrix instructions goes before the other one of its SIMD, which then does its softmax in their shadow (one sequence of 8192, above: 302, 411
+// and 601 us; without 323, 426 and 643; 8 of 1024, not causal, 16 heads of 64, forward 56 and 62).  The short kernels, whose waves wait for memory, gain nothing.
+__device__ __forceinline__ void matrix_work(bool on) {
+  if (on) __builtin_amdgcn_s_setprio(1);
+  else __builtin_amdgcn_s_setprio(0);
+}
 __device__ __forceinline__ int walked(int r, int half) { return 8 * (r >> 2) + 4 * half + (r & 3); }
 
 // A lane's values for 32 walked rows as the B operand of two products over 16 of them each, in the order of products().
@@ -378,7 +384,9 @@ struct Forward {
     constexpr int SUB = 32 * Layout<DP>::PITCH;
     const int half = (threadIdx.x & 63) >> 5;
     f32x16 s[SUBS];
+    if (SUBS > 1) matrix_work(true);
     products<DP, SUBS, SUB>(s, lds_k, [&](int, int k, int) { return q.f[k]; });
+    if (SUBS > 1) matrix_work(false);
     if (edge) {
       int most = last - j - 4 * half;
       asm volatile("" : "+v"(most));             // keeps the branch: as selects every tile would pay for it
@@ -416,8 +424,10 @@ struct Forward {
       w[n] = rounded(s[n]);
     }
     total += sum[0] + sum[1];
+    if (SUBS > 1) matrix_work(true);
 #pragma unroll
     for (int n = 0; n < SUBS; ++n) accumulate<DP, 1, 0>({&acc}, lds_v + n * SUB, {w[n]});
+    if (SUBS > 1) matrix_work(false);
   }
 };
 
@@ -557,7 +567,9 @@ __device__ __forceinline__ void queries_tile(const Args& a, const Tile& t, int h
       if (j >= seen) break;
       const char* lds_k = lds + turn + set * S::SHARE + sub * Layout<DP>::PITCH;
       f32x16 s[2];                                                  // scores, and dP
+      matrix_work(true);
       products<DP, 2, S::TILE>(s, lds_k, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
+      matrix_work(false);
       if (j + 32 > whole) {
         int most = last - j - 4 * half;
         asm volatile("" : "+v"(most));
@@ -567,7 +579,9 @@ __device__ __forceinline__ void queries_tile(const Args& a, const Tile& t, int h
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2)) * (s[1][r] - delta);
+      matrix_work(true);
       accumulate<DP, 1, 0>({&acc}, lds_k, {rounded(s[0])});
+      matrix_work(false);
     }
     if (more) {
       sk.put(lds + (turn ^ 2 * S::TILE));
@@ -663,10 +677,12 @@ __device__ __forceinline__ void keys_tile(const Args& a, const Tile& t, int kv, 
     const int from = at + 32 * set;
     if (first < t.len && from < t.len && !(a.causal && from + 32 <= first)) {
       f32x16 s[2];                                                  // scores, and dP
+      matrix_work(true);
       products<DP, 2, TILE>(s, now + set * SUB, [&](int which, int p, int base) {
         if (!which) return k.f[p];
         return V_IN_LDS ? *reinterpret_cast<const bf16x8*>(own_v + (base ^ p << 5)) : v.f[p];
       });
+      matrix_work(false);
       if (a.causal && from < first + 31) {
         int least = mine - from - 4 * half;
         asm volatile("" : "+v"(least));
@@ -685,7 +701,9 @@ __device__ __forceinline__ void keys_tile(const Args& a, const Tile& t, int kv, 
           s[1][r] = s[0][r] * (s[1][r] - d[e]);
         }
       }
+      matrix_work(true);
       accumulate<DP, 2, TILE>({&dk, &dv}, now + set * SUB, {rounded(s[1]), rounded(s[0])});
+      matrix_work(false);
     }
     at += WALK;
     if (at >= t.len) at = begin;
@@ -1009,7 +1027,7 @@ bool few(const Args& a, int heads) {
 }
 
 // Two sets of waves for tiles of 128 rows, where there are at most 3 halves (causal, with half the work: 3) of them for a compute unit: dk and dv of one sequence of 8192, causal,
-// head width 128, 16 heads on 8 of keys: 630 us against 928 with one set; on 16 of keys, two workgroups of one set a unit, 640 against 585.  Forward, 12 causal
+// head width 128, 16 heads on 8 of keys: 600 us against 928 with one set; on 16 of keys, two workgroups of one set a unit, 640 against 585.  Forward, 12 causal
 // sequences of 1 to 2048, 16 heads of 128: 43 against 52, 24 of them 143 against 112; 16 of 1 to 4096, 8 heads of 64: 57 against 74.
 template <int WAVES>
 bool two_sets(const Args& a, int heads) { return WAVES > 1 && a.tokens / (32 * WAVES) * heads / (a.causal ? 2 : 1) <= COMPUTE_UNITS * 3 / 2; }
