@@ -12,7 +12,7 @@
 // Two kernels for the backward pass instead of one: each gradient is summed by one wave in a fixed order, in registers, with neither
 // atomics nor fp32 copies of dq, for 7 products instead of 5.
 //
-// Long sequences are bound by the SIMDs' issue: forward, matrix instructions take 44 % of the time and vector instructions 45 %, and with two
+// Long sequences are bound by the SIMDs' issue: forward, matrix instructions take 45 % of the time and vector instructions 46 %, and with two
 // waves a SIMD, which is what the registers allow, they overlap in part; the LDS has no conflicts.  One causal sequence of 8192, 16
 // heads of 128 on 8: forward 302 us (910 TFLOP/s of the products below the diagonal), dq 411 (1000), dk and dv 601 (915); a large product by the vendor's
 // library reaches 1150 on the same card.  Short ones are bound by memory, at the rate of a copy but for the launches.
@@ -607,7 +607,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_bwd_q_rest(Args a) {
 }
 
 // dk and dv: 32 keys a wave; the queries of all heads that share the keys are walked, head by head, 32 rows a step for each set.  Four products a pair of
-// tiles; half of a wave's time is waiting, and there is no register left to ask for operands earlier.
+// tiles; two fifths of a wave's time are waiting, and there is no register left to ask for operands earlier.
 template <int DP, int WAVES, int SETS>
 struct Keys {
   static constexpr int SUB = 32 * Layout<DP>::PITCH, WALK = 32 * SETS, TILE = SETS * SUB;
