@@ -1007,7 +1007,7 @@ unsigned rest_grid(const Args& a, int heads) {
   const int64_t groups = (2 * COMPUTE_UNITS + heads - 1) / heads, tiles = a.tokens / 128 + a.sequences;
   return (unsigned)((groups < tiles ? groups : tiles) * heads);
 }
-bool launched() { return hipGetLastError() == hipSuccess; }
+bool launched() { return hipGetLastError() == hipSuccess; }        // once a launch: asking clears the error
 
 // Sets of waves that share rows where there are few: as many as their tiles leave room for in the LDS.
 template <int DP>
@@ -1048,7 +1048,8 @@ bool forward(Args a, int tiles, hipStream_t st) {
   }
   a.above = 32 * tiles;
   with_short<DP>(tiles, [&](auto w) { k_attention_fwd_short<DP, w()><<<(unsigned)(a.sequences * a.heads), 64 * w(), 0, st>>>(a); });
-  if (!launched() || a.tokens <= a.above) return launched();
+  if (!launched()) return false;
+  if (a.tokens <= a.above) return true;
   k_attention_fwd_rest<DP><<<rest_grid(a, a.heads), 256, 0, st>>>(a);
   return launched();
 }
@@ -1075,7 +1076,8 @@ bool backward(Args a, int tiles, hipStream_t st) {
   }
   a.above = 32 * tiles;
   with_short<DP>(tiles, [&](auto w) { k_attention_bwd_short<DP, w()><<<(unsigned)(a.sequences * a.heads), 64 * ShortBwd<DP, w()>::WAVES, 0, st>>>(a); });
-  if (!launched() || a.tokens <= a.above) return launched();
+  if (!launched()) return false;
+  if (a.tokens <= a.above) return true;
   k_attention_bwd_q_rest<DP><<<rest_grid(a, a.heads), 256, 0, st>>>(a);
   if (!launched()) return false;
   k_attention_bwd_kv_rest<DP><<<rest_grid(a, a.kv_heads), 256, 0, st>>>(a);
