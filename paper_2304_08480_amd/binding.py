@@ -128,7 +128,7 @@ _lib = _load()
 
 
 def _ptr(x):
-    if x is None or type(x) is int:
+    if x is None or isinstance(x, int):
         return x
     return x.data_ptr()       # torch tensor
 
