@@ -763,6 +763,14 @@ __device__ __forceinline__ void take_rows(const char* lds, Rows<DP>& r) {
   for (int s = 0; s < DP / 16; ++s) r.f[s] = *reinterpret_cast<const bf16x8*>(lds + (base ^ s << 5));
 }
 
+// Between lanes of a wave that write rows into the LDS and lanes that read them there, either way round: what was issued before this is done before what
+// comes after it.  One wave's LDS instructions keep their order by themselves, so this is no instruction; it is what keeps the compiler to it.
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 template <int DP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void k_attention_fwd_short(Args a) {
   using S = Short<DP, WAVES>;
@@ -786,7 +794,9 @@ __global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void k_attention_fwd_
     v.fetch(a.v + row * a.v_row + kv * a.v_head, a.v_row, rows, a.head_dim);
     char *own = lds + wave * S::SUB;
     q.put(own);
+    wave_exchange();
     take_rows<DP>(own, f.q);
+    wave_exchange();
     k.put(own);
     v.put(own + S::ALL);
   }
@@ -847,10 +857,14 @@ __global__ __launch_bounds__((64 * ShortBwd<DP, TILES>::WAVES), (DP <= 64 && TIL
     Rows<DP> o;
     sq.put(own);
     sd.put(own + S::ALL);
+    wave_exchange();
     take_rows<DP>(own, q[i]);
     take_rows<DP>(own + S::ALL, dout[i]);
+    wave_exchange();
     so.put(own);
+    wave_exchange();
     take_rows<DP>(own, o);
+    wave_exchange();
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
