@@ -298,6 +298,8 @@ DISCO_API int disco_logit_scale_bwd(const float* theta, float s_max, const float
  *   those up to i if `causal`.
  * q, k, v, o and the gradients are bf16 (dtype DISCO_BF16); lse is heads x tokens fp32, kept for the backward pass.  Scores, softmax and sums are
  * fp32, the softmax values and their gradients are rounded to bf16 before they are multiplied by v, dout, k and q.
+ * Keys may be hidden by their scores (a channel of the type's lowest value, or minus infinity): a row that sees others has the results of those.  A row
+ * whose lse is beyond 2^24 ln 2 in magnitude, as one that sees nothing but such keys, adds nothing to the gradients: fp32 does not hold its P.
  * Rows before the first and behind the last sequence are neither read nor written.  A NaN or infinity stays within its sequence; inside it, one can also
  * reach rows up to 63 away that the mask hides from it, as 0 times NaN.
  * All 16 bytes aligned, strides multiples of 8; head_dim a multiple of 8 up to 128 (else DISCO_ERR_UNSUPPORTED).  tokens < 2^31,

@@ -21,6 +21,7 @@
 // divides o is taken before that rounding.
 #include "common.h"
 
+#include <float.h>
 #include <math.h>
 
 namespace disco {
@@ -36,6 +37,15 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((address_space(3))) bf16x4* lds_bf16x4;
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// Scores in base 2 from which on fp32 numbers are 2 apart.  Keys that are hidden by their scores (the type's lowest value in a channel) are far beyond it,
+// alone in a row's first tiles or in all of them.  Forward, the rounding of the reference that is taken off them would be more than exp2 holds:
+// it is taken off before they are multiplied into base 2.  Backward, lse tells the softmax of such a row no more: the row's values are taken as 0.
+constexpr float FAR = 0x1p24f;
+__device__ __forceinline__ float base2(float lse) {
+  const float x = lse * LOG2E;
+  return fabsf(x) < FAR || !(fabsf(lse) <= FLT_MAX) ? x : INFINITY;              // exp2(-inf) = 0
+}
 
 struct Args {
   int64_t tokens;
@@ -405,13 +415,23 @@ struct Forward {
     // The reference follows the maximum only when a row's has risen by 2^8 since: sums stay below 2^8 times their number of terms, bf16 values keep their
     // relative precision, and the accumulators are rescaled a few times a row instead of at every step.
     if (__any((m - top) * c > 8.f)) {
-      const float next = fmaxf(top, m), fade = __builtin_amdgcn_exp2f((top - next) * c);
+      const float next = fmaxf(top, m), fade = __builtin_amdgcn_exp2f((top - fmaxf(next, -FLT_MAX)) * c);
       top = next;
       total *= fade;
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) acc[d] *= fade;
     }
-    const float ref = top * c;
+    float ref = top * c;
+    const bool far = !(fabsf(ref) < FAR);
+    if (__any(far)) {
+      float base = far ? fmaxf(top, -FLT_MAX) : 0.f;      // minus infinity so far: such keys add nothing
+      asm volatile("" : "+v"(base));                      // keeps the branch
+#pragma unroll
+      for (int n = 0; n < SUBS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[n][r] -= base;
+      ref = far ? 0.f : ref;
+    }
     float sum[2] = {0.f, 0.f};
     Weights w[SUBS];
 #pragma unroll
@@ -544,7 +564,7 @@ __device__ __forceinline__ void queries_tile(const Args& a, const Tile& t, int h
   }
   const int64_t at = head * a.tokens + t.first + mine;
   if (there && half == 0 && set == 0) a.delta[at] = delta;
-  const float lse2 = there ? a.lse[at] * LOG2E : 0.f;
+  const float lse2 = there ? base2(a.lse[at]) : 0.f;
   const int end = a.causal && row + S::OWN < t.len ? row + S::OWN : t.len;
   const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;
   const int last = a.causal && there ? mine : t.len - 1;
@@ -652,7 +672,7 @@ __device__ __forceinline__ void keys_tile(const Args& a, const Tile& t, int kv, 
     so.put(to + TILE);
     if (threadIdx.x < WALK) {
       // rows past the last: exp2(-inf) = 0
-      reinterpret_cast<float*>(to + 2 * TILE)[threadIdx.x] = next + (int)threadIdx.x < t.len ? next_lse * LOG2E : INFINITY;
+      reinterpret_cast<float*>(to + 2 * TILE)[threadIdx.x] = next + (int)threadIdx.x < t.len ? base2(next_lse) : INFINITY;
       reinterpret_cast<float*>(to + 2 * TILE)[WALK + threadIdx.x] = next_delta;
     }
   };
@@ -838,7 +858,7 @@ __global__ __launch_bounds__((64 * ShortBwd<DP, TILES>::WAVES), (DP <= 64 && TIL
 #pragma unroll
   for (int i = 0; i < OWN; ++i) {
     const int tile = tile_of(i), mine = 32 * tile + (lane & 31);
-    lse2[i] = mine < len ? a.lse[head * a.tokens + seq + mine] * LOG2E : INFINITY;      // exp2(-inf) = 0
+    lse2[i] = mine < len ? base2(a.lse[head * a.tokens + seq + mine]) : INFINITY;      // exp2(-inf) = 0
     delta[i] = 0.f;
     Stage<DP, 32, 64> sq, sk, sv, so, sd;
     sq.init(a.q_row, a.head_dim);
