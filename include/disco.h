@@ -364,9 +364,11 @@ DISCO_API int disco_block_norm_bwd(const disco_block_norm_shape* shape, const vo
  *
  * disco_grad_norm: *norm = sqrt(sum of all squares), or with accumulate sqrt(*norm^2 + that sum), for lists that are taken in parts.  Squares are summed
  * in fp64 in a fixed order: no gradient that fp32 holds overflows or underflows, equal calls give equal bits.
- * disco_grad_clip: dst = src * min(1, max_norm / (norm + 1e-6)), in fp32, rounded to the tensor's type; dst[i] may be src[i], else they overlap nothing.
- * The norm is *given where given is not NULL (of more lists than this one, or of several GPUs), else that of src, taken by the same call.  *norm becomes
- * the norm taken either way (before clipping; norm may be given).  A norm of NaN makes every dst NaN, one of infinity makes finite gradients 0.
+ * disco_grad_clip: dst = src * min(1, max_norm / (norm + 1e-6)), in fp64, rounded to fp32 and to the tensor's type; dst[i] may be src[i], else they overlap
+ * nothing.  The norm is *given where given is not NULL (of more lists than this one, or of several GPUs), else that of src, taken by the same call.  *norm
+ * becomes the norm taken either way (before clipping; norm may be given).  A norm of NaN makes every dst NaN, one of infinity (an infinite gradient, or
+ * given) makes finite gradients 0.  A norm that is only too large for fp32 (finite gradients, together beyond 3.4e38) is stored as infinity and clipped by
+ * as it is, where the call takes it itself.
  * workspace: disco_grad_workspace_bytes(count) (0: count < 0 or > 2^20), 256-byte aligned.  max_norm > 0 (infinity: nothing is clipped).
  */
 DISCO_API size_t disco_grad_workspace_bytes(int64_t count);

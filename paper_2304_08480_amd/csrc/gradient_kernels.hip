@@ -135,29 +135,32 @@ __device__ __forceinline__ double sum_of(const double* parts, int n) {
   return block_sum(s);
 }
 
-__global__ __launch_bounds__(1024) void k_grad_norm(const double* parts, int n, int accumulate, float* norm) {
+// The sum of the squares takes the place of the first partial sum, for the product.
+__global__ __launch_bounds__(1024) void k_grad_norm(double* parts, int n, int accumulate, float* norm) {
   double s = sum_of(parts, n);
   if (threadIdx.x == 0) {
+    parts[0] = s;
     if (accumulate) s = fma((double)*norm, (double)*norm, s);
     *norm = (float)sqrt(s);
   }
 }
 
 // The pieces run from the end of a tensor (and the host's tables from the end of the list): what the norm read last is still in the last-level
-// cache.  Few partial sums (n > 0) are joined by every workgroup for itself, the norm's own launch is saved: all of them take the same order, so
-// they come to the same norm, and the first one stores it.
+// cache.  Few partial sums are joined by every workgroup for itself, the norm's own launch is saved: all of them take the same order, so
+// they come to the same norm, and the first one stores it.  Of many k_grad_norm has left one (n = 1); a given norm has none (n = 0).
+// Norm and factor are fp64 up to the product: a norm beyond fp32, of gradients that are all finite, has a factor like any other.
 __global__ __launch_bounds__(THREADS) void k_grad_scale(Table table, float max_norm, float* norm, const double* parts, int n) {
-  float taken;
+  double taken;
   if (n) {
-    taken = (float)sqrt(sum_of(parts, n));
-    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = taken;
+    taken = sqrt(n == 1 ? parts[0] : sum_of(parts, n));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)taken;
   } else {
     taken = *norm;
   }
-  const float quotient = max_norm / (taken + 1e-6f), factor = quotient < 1.f ? quotient : taken == taken ? 1.f : taken;
+  const double quotient = max_norm / (taken + 1e-6), factor = quotient < 1.0 ? quotient : taken == taken ? 1.0 : taken;
   for (int p = blockIdx.x; p < table.pieces; p += gridDim.x) {
     const Tensor& t = table.t[tensor_of(table, p)];
-    if (factor == 1.f && t.src == t.dst) continue;
+    if (factor == 1.0 && t.src == t.dst) continue;
     const int64_t from = ((t.n + PIECE - 1) / PIECE - 1 - (p - t.first)) * PIECE + threadIdx.x * 8;
     Eight r[UNROLL];
 #pragma unroll
@@ -167,7 +170,7 @@ __global__ __launch_bounds__(THREADS) void k_grad_scale(Table table, float max_n
       float v[8];
       values(r[u], t.bf16, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= factor;
+      for (int e = 0; e < 8; ++e) v[e] = (float)(v[e] * factor);
       store8(t.dst, from + u * THREADS * 8, t.n, t.bf16, v);
     }
   }
@@ -226,7 +229,7 @@ int squares(const void* const* src, const int64_t* elements, const int32_t* dtyp
   });
   return ok ? n : -1;
 }
-bool norm_of(const double* parts, int n, int accumulate, float* norm, hipStream_t st) {
+bool norm_of(double* parts, int n, int accumulate, float* norm, hipStream_t st) {
   k_grad_norm<<<1, 1024, 0, st>>>(parts, n, accumulate, norm);
   return hipGetLastError() == hipSuccess;
 }
@@ -273,7 +276,7 @@ extern "C" int disco_grad_clip(const void* const* src, void* const* dst, const i
     if (n < 0) return DISCO_ERR_HIP;
     if (n == 0 || n > FEW) {
       if (!norm_of(parts, n, 0, norm, st)) return DISCO_ERR_HIP;
-      n = 0;
+      n = 1;
     }
   } else if (given != norm) {
     k_grad_keep<<<1, 64, 0, st>>>(given, norm);

@@ -132,3 +132,25 @@ def test_captured_and_equal_bits():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(norm, size) and all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("sizes", [[1000, 24, 8000, 8193], [9_000_001, 7, 33]], ids=lambda s: f"{len(s)}x{s[0]}")
+@pytest.mark.parametrize("value,max_norm", [(3e38, 1.0), (3e38, 1e30), (1e36, 0.25), (1e-3, 0.5)])
+def test_the_factor_is_that_of_the_norm_in_fp64(sizes, value, max_norm):
+    """Finite gradients are clipped by their norm, also by one that fp32 does not hold.  Sums of 10^7 squares in fp64 leave 2^-30 at the very most in
+    the factor, fp32 2^-24 in the product, the type's half step on top where it is narrower; below fp32's normal numbers half of 2^-149."""
+    print("case clip factor", sizes, value, max_norm, flush=True)
+    grads = [g.mul_(value / 4).clamp_(-value, value) for g in _grads(sizes, seed=11)]
+    ws, need = _workspace(len(grads))
+    norm = torch.full((1,), float("nan"), device="cuda")
+    outs = [torch.full_like(g, float("nan")) for g in grads]
+    dl.disco_grad_clip(grads, outs, max_norm, None, norm, ws, need, torch.cuda.current_stream())
+    want = _norm(grads)
+    assert float(norm) == (math.inf if want > 3.41e38 else pytest.approx(want, rel=2.0 ** -23))
+    factor = min(1.0, float(torch.tensor(max_norm, dtype=torch.float32)) / (want + 1e-6))      # max_norm is a C float
+    for g, o in zip(grads, outs):
+        exact = g.double() * factor
+        step = 2.0 ** -24 + (STEP[g.dtype] if g.dtype != torch.float32 else 0.0) + 2.0 ** -30
+        assert float(((o.double() - exact).abs() - exact.abs() * step).max()) <= 2.0 ** -150, factor
+    dl.disco_grad_clip(grads, grads, max_norm, None, norm, ws, need, torch.cuda.current_stream())      # in place
+    assert all(torch.equal(a, b) for a, b in zip(grads, outs))
