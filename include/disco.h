@@ -303,7 +303,7 @@ DISCO_API int disco_logit_scale_bwd(const float* theta, float s_max, const float
  * Rows before the first and behind the last sequence are neither read nor written.  A NaN or infinity stays within its sequence; inside it, one can also
  * reach rows up to 63 away that the mask hides from it, as 0 times NaN.
  * All 16 bytes aligned, strides multiples of 8; head_dim a multiple of 8 up to 128 (else DISCO_ERR_UNSUPPORTED).  tokens < 2^31,
- * sequences <= 2^24, heads <= 2^16, (tokens / 32 + 8 sequences) heads < 2^26, scale > 0, row strides in 1 .. 2^22, head strides
+ * sequences <= 2^24, heads <= 2^16, (tokens / 32 + 8 sequences) heads < 2^26, scale > 0 and scale log2(e) finite, row strides in 1 .. 2^22, head strides
  * in 1 .. 2^40 (else DISCO_ERR_SHAPE).  Outputs overlap
  * nothing else (q, k, v may be views of one buffer, and so may dq, dk, dv).  Equal calls give equal bits.
  *

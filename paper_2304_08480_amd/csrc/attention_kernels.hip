@@ -976,7 +976,7 @@ __global__ __launch_bounds__((64 * ShortBwd<DP, TILES>::WAVES), (DP <= 64 && TIL
 int check(const disco_attention_shape* s) {
   if (!s) return DISCO_ERR_NULL;
   if (s->tokens <= 0 || s->tokens > 0x7fffffff || s->sequences <= 0 || s->sequences > 1 << 24 || s->heads <= 0 || s->kv_heads <= 0 ||
-      s->heads > 1 << 16 || s->heads % s->kv_heads != 0 || s->head_dim <= 0 || !(s->scale > 0.f) || !isfinite(s->scale))
+      s->heads > 1 << 16 || s->heads % s->kv_heads != 0 || s->head_dim <= 0 || !(s->scale > 0.f) || !isfinite(s->scale * LOG2E))
     return DISCO_ERR_SHAPE;
   // a launch has less than 2^32 threads: 64 for a tile of 32 rows, up to 512 for a sequence
   if ((s->tokens / 32 + (int64_t)s->sequences * 8) * s->heads >= (int64_t)1 << 26) return DISCO_ERR_SHAPE;

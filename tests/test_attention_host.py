@@ -62,3 +62,10 @@ def test_beyond_the_32_bits_of_a_tile_s_addresses_and_of_a_launch(kw):
 def test_the_largest_row_stride_and_launch():
     assert dl.disco_attention_workspace_bytes(_shape(q_row=1 << 22, k_row=1 << 22, v_row=1 << 22, o_row=1 << 22)) > 0
     assert dl.disco_attention_workspace_bytes(_shape(sequences=(1 << 20) - 1)) > 0
+
+
+def test_scales_past_fp32_in_base_2():
+    # scores are taken times scale log2(e): 2.4e38 is fp32, its product is not, and 0 times that would be NaN
+    assert set(_calls(_shape(scale=2.4e38))) == {dl.DISCO_ERR_SHAPE}
+    assert dl.disco_attention_workspace_bytes(_shape(scale=2.4e38)) == 0
+    assert dl.disco_attention_workspace_bytes(_shape(scale=2.3e38)) > 0
