@@ -297,7 +297,8 @@ DISCO_API int disco_logit_scale_bwd(const float* theta, float s_max, const float
  *   o_i = sum_j P_ij v_j,  P_ij = exp(scale <q_i, k_j> - lse_i),  lse_i = log sum_j exp(scale <q_i, k_j>),  over the keys j of row i's sequence,
  *   those up to i if `causal`.
  * q, k, v, o and the gradients are bf16 (dtype DISCO_BF16); lse is heads x tokens fp32, kept for the backward pass.  Scores, softmax and sums are
- * fp32, the softmax values and their gradients are rounded to bf16 before they are multiplied by v, dout, k and q.
+ * fp32, the softmax values and their gradients are rounded to bf16 before they are multiplied by v, dout, k and q.  The backward pass takes <dout, o> from o as
+ * stored, but for rows whose keys are all among the first 32 of the sequence, where its rounding weighs most.
  * Keys may be hidden by their scores (a channel of the type's lowest value, or minus infinity): a row that sees others has the results of those.  A row
  * whose lse is beyond 2^24 ln 2 in magnitude, as one that sees nothing but such keys, adds nothing to the gradients: fp32 does not hold its P.
  * Rows before the first and behind the last sequence are neither read nor written.  A NaN or infinity stays within its sequence; inside it, one can also

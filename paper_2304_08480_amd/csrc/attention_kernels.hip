@@ -534,6 +534,17 @@ __global__ __launch_bounds__(256, 2) void k_attention_fwd_rest(Args a) {
   each_rest<128, false>(a, blockIdx.x / a.heads, gridDim.x / a.heads, [&](const Tile& t) { forward_tile<DP, 4, 1>(a, t, blockIdx.x % a.heads, lds); });
 }
 
+// delta of a row all of whose keys are in one tile: sum P dP, which is <do, o> without the roundings of o to bf16 and of P on the way to it.  They are
+// shared by all of a row's dS, and weigh most where its keys are few: a row of one key has no dq and adds nothing to its dk.  (Relative errors of dq and dk
+// against 64 bits, packed causal batches of mean lengths from 10 to 60: 0.0024 for 0.0028 to 0.0032; of 0.0017 that is the rounding of dq and dk themselves.
+// Rows of more keys would take a second walk, and lose little without it.)
+__device__ __forceinline__ float own_delta(const f32x16& p, const f32x16& dp) {
+  float d = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) d = fmaf(p[r], dp[r], d);
+  return d + other_half(d);
+}
+
 // dq, and delta = <do, o> of every row for the kernel of dk and dv, which runs after this one.  Three products a pair of tiles, S and dP with shared addresses.
 template <int DP, int WAVES, int SETS>
 __device__ __forceinline__ void queries_tile(const Args& a, const Tile& t, int head, char* lds) {
@@ -563,7 +574,6 @@ __device__ __forceinline__ void queries_tile(const Args& a, const Tile& t, int h
     delta += other_half(delta);
   }
   const int64_t at = head * a.tokens + t.first + mine;
-  if (there && half == 0 && set == 0) a.delta[at] = delta;
   const float lse2 = there ? base2(a.lse[at]) : 0.f;
   const int end = a.causal && row + S::OWN < t.len ? row + S::OWN : t.len;
   const int seen = first >= t.len ? 0 : a.causal && first + 32 < t.len ? first + 32 : t.len;
@@ -598,7 +608,10 @@ __device__ __forceinline__ void queries_tile(const Args& a, const Tile& t, int h
           if (walked(r, 0) > most) s[0][r] = -INFINITY;
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2)) * (s[1][r] - delta);
+      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2));
+      if (seen <= 32) delta = own_delta(s[0], s[1]);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[0][r] *= s[1][r] - delta;
       matrix_work(true);
       accumulate<DP, 1, 0>({&acc}, lds_k, {rounded(s[0])});
       matrix_work(false);
@@ -611,6 +624,7 @@ __device__ __forceinline__ void queries_tile(const Args& a, const Tile& t, int h
   }
   join<DP, WAVES, SETS>(lds, wave, set, acc);
   if (set) return;
+  if (there && half == 0) a.delta[at] = delta;
   store_row<DP>(a.dq + (t.first + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, there);
 }
 
@@ -914,7 +928,10 @@ __global__ __launch_bounds__((64 * ShortBwd<DP, TILES>::WAVES), (DP <= 64 && TIL
           if (walked(r, 0) > most) s[0][r] = -INFINITY;
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2[i])) * (s[1][r] - delta[i]);
+      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2[i]));
+      if (end == 1) delta[i] = own_delta(s[0], s[1]);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[0][r] *= s[1][r] - delta[i];
       accumulate<DP, 1, 0>({&acc}, now, {rounded(s[0])});
     }
     store_row<DP>(a.dq + (seq + mine) * a.q_row + head * a.q_head, acc, a.scale, a.head_dim, mine < len);
