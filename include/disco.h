@@ -303,7 +303,7 @@ DISCO_API int disco_logit_scale_bwd(const float* theta, float s_max, const float
  * whose lse is beyond 2^24 ln 2 in magnitude, as one that sees nothing but such keys, adds nothing to the gradients: fp32 does not hold its P.
  * Rows before the first and behind the last sequence are neither read nor written.  A NaN or infinity stays within its sequence; inside it, one can also
  * reach rows up to 63 away that the mask hides from it, as 0 times NaN.
- * All 16 bytes aligned, strides multiples of 8; head_dim a multiple of 8 up to 128 (else DISCO_ERR_UNSUPPORTED).  tokens < 2^31,
+ * All 16 bytes aligned, strides multiples of 8; head_dim a multiple of 8 up to 128 (else DISCO_ERR_UNSUPPORTED).  1 <= tokens < 2^31,
  * sequences <= 2^24, heads <= 2^16, (tokens / 32 + 8 sequences) heads < 2^26, scale > 0 and scale log2(e) finite, row strides in 1 .. 2^22, head strides
  * in 1 .. 2^40 (else DISCO_ERR_SHAPE).  Outputs overlap
  * nothing else (q, k, v may be views of one buffer, and so may dq, dk, dv).  Equal calls give equal bits.
@@ -339,7 +339,8 @@ DISCO_API int disco_attention_bwd(const disco_attention_shape* shape, const int3
  * forward call (those that the formulas use: y and dn with a norm before the next block, h with a norm after the block or a gate).  Writes dx (NULL: not wanted), dh, and where not NULL dgate (as gate), dw_post, db_post, dw_pre, db_pre: sums over all rows, in a fixed
  * order (equal calls give equal bits).  workspace: disco_block_norm_workspace_bytes (0: invalid shape), 256-byte aligned.
  * Each row's loads come before its stores, so in either call an output may be one of its inputs of the same type (y = x, n = h, dx = dy, dh = dn).
- * A NaN or infinity stays within its row, and in the sums over rows.
+ * A NaN or infinity stays within its row, and in the sums over rows.  Statistics are fp32: a row's sum of squares (of deviations from its mean) has to be a
+ * number there (as of 8192 values up to 2 10^17), and with eps = 0 a normal one.
  */
 typedef enum { DISCO_NORM_NONE = 0, DISCO_NORM_LAYER = 1, DISCO_NORM_RMS = 2 } disco_norm;
 typedef enum { DISCO_GATE_NONE = 0, DISCO_GATE_CHANNEL = 1 /* d fp32 */, DISCO_GATE_ELEMENT = 2 /* rows x d */ } disco_gate;

@@ -14,11 +14,13 @@
 //
 // Long sequences are bound by the SIMDs' issue: forward, matrix instructions take 45 % of the time and vector instructions 46 %, and with two
 // waves a SIMD, which is what the registers allow, they overlap in part; the LDS has no conflicts.  One causal sequence of 8192, 16
-// heads of 128 on 8: forward 302 us (910 TFLOP/s of the products below the diagonal), dq 411 (1000), dk and dv 601 (915); a large product by the vendor's
-// library reaches 1150 on the same card.  Short ones are bound by memory, at the rate of a copy but for the launches.
+// heads of 128 on 8: forward 303 us (905 TFLOP/s of the products below the diagonal), dq 410 (1005), dk and dv 598 (920); a large product by the vendor's
+// library reaches 1150 on the same card.  What bounds short ones stands at their kernels.
 //
-// Scores, statistics and sums are fp32.  P and dS are rounded to bf16 (by at most 2^-8 of each value) for the matrix instruction; the sum of P that
-// divides o is taken before that rounding.
+// Scores, statistics and sums are fp32.  P and dS are rounded to bf16 (by at most 2^-8 of each value) for the matrix instruction, whose fp32 form has a
+// sixteenth of the rate; in two bf16 parts each they would take one product more forward, of 2, and three more backward, of 7.  The sum of P that
+// divides o is taken before that rounding.  delta is taken from o as stored, but for rows of few keys (own_delta).  Against 64 bits o is off by 0.0020 to
+// 0.0025 of its norm and the gradients by 0.0022 to 0.0025, 0.0017 of which is their own rounding to bf16.
 #include "common.h"
 
 #include <float.h>
@@ -767,9 +769,11 @@ __global__ __launch_bounds__(256, 2) void k_attention_bwd_kv_rest(Args a) {
 // wave, 16 bytes a lane at a time, which is also how it goes into the LDS for the other waves; there is no walk to be kept supplied, no search for
 // the tile, and the backward pass is one kernel: the queries' side first, then the waves put queries and do in the place of keys and values.
 //
-// Bound by memory: 1024 captions of up to 77 tokens, causal, 8 heads of 64, 23 us forward and 47 backward; 128 x 197 patches, 12 heads of 64, 42 (155 MB, 3.7
-// TB/s) and 114 to 121 (310 MB, 2.6 to 2.7 TB/s).  What goes to memory next is read a whole tile of rows at a time (rows by the lanes that own them, 32
-// bytes of each at once, took 43 for 36 in the backward kernel of captions of up to 64).
+// A few tiles are bound by memory: 1024 captions of up to 77 tokens, causal, 8 heads of 64, 23 us forward and 47 backward, the rate of a copy.  Many are
+// not: 128 x 197 patches, 12 heads of 64, take 41 to 45 (155 MB, 3.4 to 3.8 TB/s) and 113 to 120 (310 MB, 2.6 to 2.7 TB/s), where a workgroup
+// reads, computes and stores one behind the other with one more on its compute unit to fill in: backward 1.5 waves a SIMD, a third of their time waiting, vector
+// instructions 40 % of the time (S, dP and the exponentials are taken twice), matrix instructions 27 %.  Rows are read a whole tile at a time (by the
+// lanes that own them, 32 bytes of each at once, they took 43 for 36 in the backward kernel of captions of up to 64).
 template <int DP, int WAVES>
 struct Short {
   static constexpr int ROWS = 32 * WAVES, SUB = 32 * Layout<DP>::PITCH, ALL = WAVES * SUB;
@@ -1028,7 +1032,11 @@ constexpr int COMPUTE_UNITS = 256;
 // the mean where that is at most the widest: few sequences are longer (of lengths spread evenly over the decades from 4 to 77 the longest is 3.1 times the
 // mean), and tiles that are not there cost the rest occupancy.  Forward and backward, 8 heads of 64: 500 sequences of 44, 63 us with 4 tiles, 79 with 6, 84
 // without these kernels; 400 of 8 to 120, 59, 72 and 74; 150 of 4 to 77, 23 with 3 tiles, 51 with 2, which leave some.  The widest up to 4/5 of it:
-// sequences of one length, as images have (128 x 197, 12 heads: 160 against 220 without).
+// sequences of one length, as images have (128 x 197, 12 heads: 150 against 220 without).
+//
+// Short sequences of one length get more tiles than they fill by this, which goes by lengths that are spread.  Kernels forward and backward, heads of 64, tiles
+// taken and tiles that they need: 512 x 50 on 12 heads 134 us with 6, 108 with 2; 1024 x 77, causal, on 8 heads 310 with 8, 270 with 3; 512 x 77 on 8 heads 151
+// and 122; 512 x 96 on 12 heads 265 and 228; 256 x 128 on 12 heads 167 with 8, 143 with 4.  Only the longest length would tell, which the host does not have.
 //
 // None for few sequences of narrow heads that are short or, as causal ones mostly are, of different lengths: these kernels are five launches for three, and what
 // they leave then takes longest.  Forward and backward, with them and without: 150 of 4 to 77 on 8 heads, 32 and 25 us where the host is the slower, 23 and

@@ -4,9 +4,10 @@
 //   t = dy + N_pre'(dn),  dx = x_scale t,  du = h_scale gate t,  dh = N_post'(du),  dgate = h_scale t u
 //   N'(g) = rstd (a - [mean a] - zhat mean(a zhat)),  a = g w,  zhat = (z - mean) rstd;  dw = sum over rows g zhat,  db = sum over rows g
 //
-// Bound by memory, and within a tenth of it but for the widest shares of idle lanes (forward 39424 x 512 bf16, a norm before: 32 us, 5.0 TB/s; 10007 x 1001
-// fp32, both norms, an element gate: 42 us, 4.8 TB/s; backward 16384 x 4096, fp32 stream, bf16 branch, both norms: 271 us, 4.5 TB/s; 50432 x 768
-// bf16, where a quarter of the lanes have no columns: 133 us, 3.5 TB/s).  A row is read once, kept in registers (8 columns a lane, LANES lanes a row, so that rows of a few hundred columns
+// Bound by memory up to 4096 columns (forward 39424 x 512 bf16, a norm before: 32 us, 5.0 TB/s; 10007 x 1001
+// fp32, both norms, an element gate: 42 us, 4.8 TB/s; backward 16384 x 4096, fp32 stream, bf16 branch, both norms: 249 to 256 us, 4.8 TB/s; 50432 x 768
+// bf16, where a quarter of the lanes have no columns: 133 us with the sums' kernel, 3.5 TB/s; a large copy reaches 4.7, calls that read more than they write
+// more).  Wider rows with both norms are not, backward (see waves_bwd).  A row is read once, kept in registers (8 columns a lane, LANES lanes a row, so that rows of a few hundred columns
 // share a wave and the widest take 16) and written once.  The variance is summed over the deviations from the mean, which are at
 // hand, not taken as a difference of sums.  The backward pass adds the sums over rows up in registers, one workgroup's rows in the LDS, and
 // the workgroups' in a second kernel, in a fixed order.  Everything is fp32 but what is stored.
@@ -224,6 +225,8 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256, (waves_fwd<POST, PRE>())
 
 // Waves a SIMD that the backward kernel's registers are kept to: what hides its loads is other rows' waves (50432 x 768 bf16, a norm before the next
 // block, a gate for each channel: 204 us with 3 waves, 140 with 4; asking for the next row's data a row ahead costs the registers of a wave and 180).
+// Rows of more than 4096 columns are workgroups of 1024 lanes, 4 waves a SIMD whatever this says: 128 registers, of which both norms' parameters and sums
+// need more.  64 (all bf16) and 83 are kept in memory, and 8192 x 8192 take 385 us with an fp32 stream (3.1 TB/s) and 460 in bf16 (1.8 TB/s).
 template <bool POST, bool PRE, bool NARROW>
 constexpr int waves_bwd() { return POST && PRE ? (NARROW ? 3 : 2) : NARROW ? 4 : 3; }
 

@@ -4,7 +4,7 @@
 // and sizes travel as kernel arguments, TABLE tensors a launch, so that a call copies nothing to the device, can be captured, and depends on no
 // memory of the host's after it returns.  Inside a launch the tensors are cut into pieces of PIECE elements, dealt to the workgroups in turn,
 // so that a launch is as even with one large tensor as with a hundred small ones.  150 million fp32 gradients in 292 tensors, three launches of either
-// kernel: squares 130 us (4.6 TB/s), products 226 (5.3 TB/s), 5 for the sum of the squares between them; a few gradients in 4 tensors: 15 us, the launches.
+// kernel: squares 132 us (4.5 TB/s), products 230 (5.2 TB/s), 5 for the sum of the squares between them; a few gradients in 4 tensors: 15 us, the launches.
 //
 // Squares are summed in fp64: a tower's 10^8 of them lose nothing, and the rate of fp64 is far above that of the memory.
 #include "common.h"
