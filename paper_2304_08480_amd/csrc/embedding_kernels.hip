@@ -37,41 +37,29 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int64_t i, int wide) {
   return wide ? static_cast<const int64_t*>(ids)[i] : static_cast<const int32_t*>(ids)[i];
 }
 
-// Rows that a group of lanes asks for at once.  Waves enough are on the chip to keep the memory busy with one each: 26 thousand rows of 512 forward and backward
-// 72.5 us, with two 72.7, with four 74.0, with eight 78.
-constexpr int THREADS = 256, AHEAD = 1;
-// A row's lanes, LANES of 8 columns each.
+constexpr int THREADS = 256;
+// A row's lanes, LANES of 8 columns each.  One row at a time for a group of lanes: waves enough are on the chip to keep the memory busy with one each (26 thousand rows
+// of 512 forward and backward 72.5 us, with two rows asked for at once 72.7, with four 74.0, with eight 78).
 template <bool TABLE_BF16, bool Y_BF16, int LANES, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void k_embedding(Lookup a) {
   constexpr int GROUPS = THREADS / LANES;
   const int lane = threadIdx.x % LANES;
-  const int64_t first = ((int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES) * AHEAD;
-  int64_t id[AHEAD], place[AHEAD];
-#pragma unroll
-  for (int u = 0; u < AHEAD; ++u) {
-    const bool there = first + u < a.rows;
-    id[u] = there ? id_at(a.ids, first + u, a.wide_ids) : -1;
-    place[u] = there && a.places ? id_at(a.place, first + u, a.wide_ids) : -1;
-    if (id[u] >= a.vocabulary) id[u] = -1;
-    if (place[u] >= a.places) place[u] = -1;
-  }
-  for (int col = lane * 8; col < a.d; col += LANES * 8) {
-    Eight<TABLE_BF16> e[AHEAD], p[AHEAD];
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      e[u].clear();
-      p[u].clear();
-      if (id[u] >= 0) e[u].template load<WHOLE>(a.table, id[u] * a.d, col, a.d);
-      if (place[u] >= 0) p[u].template load<WHOLE>(a.place_table, place[u] * a.d, col, a.d);
-    }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
+  for (int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * GROUPS) {
+    int64_t id = id_at(a.ids, row, a.wide_ids), place = a.places ? id_at(a.place, row, a.wide_ids) : -1;
+    if (id >= a.vocabulary) id = -1;
+    if (place >= a.places) place = -1;
+    for (int col = lane * 8; col < a.d; col += LANES * 8) {
+      Eight<TABLE_BF16> e, p;
+      e.clear();
+      p.clear();
+      if (id >= 0) e.template load<WHOLE>(a.table, id * a.d, col, a.d);
+      if (place >= 0) p.template load<WHOLE>(a.place_table, place * a.d, col, a.d);
       float v[8];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) v[c] = fmaf(a.scale, id[u] >= 0 ? e[u].value(c) : 0.f, p[u].value(c));
+      for (int c = 0; c < 8; ++c) v[c] = fmaf(a.scale, id >= 0 ? e.value(c) : 0.f, p.value(c));
       Eight<Y_BF16> y;
       y.set(v);
-      if (first + u < a.rows) y.template store<WHOLE>(a.y, (first + u) * a.d, col, a.d, a.stream);
+      y.template store<WHOLE>(a.y, row * a.d, col, a.d, a.stream);
     }
   }
 }
@@ -575,6 +563,8 @@ int check(const disco_embedding_shape* s) {
 }
 
 bool aligned(const void* p, int n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+// Workgroups of a lookup.  A launch has less than 2^32 threads, which from 2^26 rows on a group of lanes for each would pass: they take more rows each then.
+constexpr int64_t MOST_LOOKUP = ((int64_t)1 << 31) / THREADS;
 // Rows of more bytes are written past the caches: smaller ones are found there by what reads them next, larger ones only drive out the table.  Rows of 2048,
 // with a copy of them behind it: 64 MiB 53.9 us and 49.2 as they come (17.5 and 26.2 alone), 80 MiB 66.1 and 67.3 (21.1, 35.1), 128 MiB 102 and 113 (31, 54).
 constexpr int64_t STREAM_ROWS = (int64_t)72 << 20;
@@ -647,8 +637,9 @@ extern "C" int disco_embedding_fwd(const disco_embedding_shape* shape, const voi
     return with_bool(s.table_dtype == DISCO_BF16, [&](auto tb) {
       return with_bool(s.y_dtype == DISCO_BF16, [&](auto yb) {
         return with_bool(s.d % 8 == 0, [&](auto whole) {
-          constexpr int ROWS = THREADS / lanes() * AHEAD;
-          k_embedding<tb(), yb(), lanes(), whole()><<<(unsigned)((s.rows + ROWS - 1) / ROWS), THREADS, 0, st>>>(a);
+          constexpr int ROWS = THREADS / lanes();
+          const int64_t all = (s.rows + ROWS - 1) / ROWS;
+          k_embedding<tb(), yb(), lanes(), whole()><<<(unsigned)(all < MOST_LOOKUP ? all : MOST_LOOKUP), THREADS, 0, st>>>(a);
           return launched();
         });
       });
