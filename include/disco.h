@@ -299,8 +299,9 @@ DISCO_API int disco_logit_scale_bwd(const float* theta, float s_max, const float
  * q, k, v, o and the gradients are bf16 (dtype DISCO_BF16); lse is heads x tokens fp32, kept for the backward pass.  Scores, softmax and sums are
  * fp32, the softmax values and their gradients are rounded to bf16 before they are multiplied by v, dout, k and q.  The backward pass takes <dout, o> from o as
  * stored, but for rows whose keys are all among the first 32 of the sequence, where its rounding weighs most.
- * Keys may be hidden by their scores (a channel of the type's lowest value, or minus infinity): a row that sees others has the results of those.  A row
- * whose lse is beyond 2^24 ln 2 in magnitude, as one that sees nothing but such keys, adds nothing to the gradients: fp32 does not hold its P.
+ * Keys may be hidden by their scores (a channel of the type's lowest value, or products past fp32's range, so that scores are minus infinity): a row that sees others has
+ * the results of those.  A row whose lse is beyond 2^24 ln 2 in magnitude, as one that sees nothing but keys of the type's lowest value, adds nothing to the gradients: fp32
+ * does not hold its P.  A row with no score above minus infinity has no softmax: its o is NaN, as are gradients that it has part in.  An infinity in k hides its key in o and lse alike, but dq is NaN in that channel (0 times it).
  * Rows before the first and behind the last sequence are neither read nor written.  A NaN or infinity stays within its sequence; inside it, one can also
  * reach rows up to 63 away that the mask hides from it, as 0 times NaN.
  * All 16 bytes aligned, strides multiples of 8; head_dim a multiple of 8 up to 128 (else DISCO_ERR_UNSUPPORTED).  1 <= tokens < 2^31,
@@ -442,10 +443,11 @@ DISCO_API int disco_head_norm_bwd(const disco_head_norm_shape* shape, const int3
  * Rows q_starts[s] .. q_starts[s + 1] of q and o are the queries of sequence s, rows k_starts[s] .. k_starts[s + 1] of k and v its keys (both: sequences + 1
  * int32 on the device, as disco_attention's starts; either side of a sequence may be empty).  Every query sees all keys of its sequence:
  *   o_i = sum_j P_ij v_j,  P_ij = exp(scale <q_i, k_j> - lse_i),  lse_i = log sum_j exp(scale <q_i, k_j>)
- * A query that sees no key, or none whose score is not minus infinity, has o = 0 and lse = -infinity, no gradient and no part in those of the keys.
+ * A query that sees no key, or none whose score is not minus infinity, has o = 0 and lse = -infinity, no gradient and no part in those of the keys.  A key whose score
+ * is minus infinity has none from that query and no part in the query's, whether the score comes from products past fp32's range or from an infinite channel of k or q.
  * q_longest, k_longest: no sequence has more queries, keys than that (0: not known).  It makes the call faster; a sequence that is longer all the same is taken
  * up to there, and what lies behind is neither read nor written.
- * Types, roundings, key/value heads shared by query heads, element strides, alignments, head widths, hidden keys, rows of no sequence, what overlaps, and that
+ * Types, roundings, key/value heads shared by query heads, element strides, alignments, head widths, keys hidden by the type's lowest value, rows of no sequence, what overlaps, and that
  * equal calls give equal bits, are as for disco_attention; <dout, o> is taken from o as stored, but for sequences of up to 32 keys.  A NaN or infinity stays
  * within its sequence, and can there reach all its rows.
  * 1 <= q_tokens, k_tokens < 2^31, q_tokens heads / kv_heads < 2^31 - 512, sequences <= 2^24, heads <= 2^16, (tokens / 32 + 8 sequences) heads < 2^26 for either side's

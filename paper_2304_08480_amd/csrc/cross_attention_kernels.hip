@@ -191,6 +191,60 @@ __device__ __forceinline__ void store_rows(char* lds, __bf16* to, int64_t pitch,
 // Backward, lse of a row that sees no key, or none that is not hidden by its score, says the same as one too large to be held: its values are 0.
 __device__ __forceinline__ float row_base2(float lse) { return lse == -INFINITY ? INFINITY : base2(lse); }
 
+// Backward, a score of minus infinity has P = dS = 0.  If it comes from an infinite channel of its key or query, that channel must not be multiplied by the 0: for the
+// products with dS infinities count as zeros.  It changes nothing else, as every score that an infinity is in is infinite or no number, with a dS that is 0 or no
+// number.  A wave that has a tile for itself looks at its scores, and takes the infinities out of the tile once they are taken.  Waves that share a tile look at their accumulators
+// at the end, and walk again if there is no number among them.  Forward and backward, microseconds without / with that: 256 captions 143 / 139 (a register less, and a third
+// wave), latents 146 / 149, 100 times 40 queries over 197 rows, 8 heads of 128, 93 / 96, 2 x 3000 on 3000, 8 heads of 64, 241 / 244, the pooled images 182 / 180.
+// (Two forms of the product, one for either case, spill registers in every walk: the accumulators stand elsewhere in each.)
+// ROWS rows of a tile in the LDS, by THREADS threads.
+template <int DP, int ROWS, int THREADS>
+__device__ __forceinline__ void without_infinities(char* lds) {
+  using L = Layout<DP>;
+  wave_exchange();
+#pragma unroll 1
+  for (int id = threadIdx.x % THREADS; id < ROWS * L::PIECES; id += THREADS) {
+    u32x4* const at = reinterpret_cast<u32x4*>(lds + L::at(id / L::PIECES, id % L::PIECES));
+    u32x4 w = *at;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((w[e] & 0x7fffu) == 0x7f80u) w[e] &= 0xffff0000u;
+      if ((w[e] & 0x7fff0000u) == 0x7f800000u) w[e] &= 0xffffu;
+    }
+    *at = w;
+  }
+  wave_exchange();
+}
+// Whether some lane's scores are minus infinity.
+__device__ __forceinline__ bool hidden(const f32x16& s) {
+  float m = s[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) m = fminf(m, s[r]);
+  return __any(m == -INFINITY);
+}
+// Whether a lane has accumulated something that is no number (or infinities that would come to one).
+template <int N>
+__device__ __forceinline__ bool no_number(const f32x16 (&acc)[N]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int m = 0; m < N; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum += acc[m][r];
+  return sum != sum;
+}
+// Whether any lane of the workgroup says so.
+template <int WAVES>
+__device__ __forceinline__ bool any_lane(bool v, int32_t (&said)[WAVES]) {
+  int32_t all = __any(v);
+  if (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) said[threadIdx.x >> 6] = all;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) all |= said[w];
+  }
+  return __builtin_amdgcn_readfirstlane(all) != 0;
+}
+
 // ---- forward
 
 template <int DP, int WAVES>
@@ -338,8 +392,10 @@ __global__ __launch_bounds__(256) void k_cross_join_rows(Args a) {
 
 // ---- backward
 
+// A wave alone with 128 channels may have more than half of a SIMD's registers: the LDS has room for five of them on a compute unit, not eight (captions of 22 on average over 197
+// rows, 8 heads of 128, forward and backward: 145 us, 176 with some registers in memory).
 template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_cross_bwd_q(Args a) {
+__global__ __launch_bounds__(64 * WAVES, WAVES == 1 && DP == 128 ? 1 : 2) void k_cross_bwd_q(Args a) {
   using S = Shape<DP, WAVES, 1>;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS];
   Walk w;
@@ -355,7 +411,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cross_bwd_q(Args a) {
   sv.init(a.v_row, a.head_dim);
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = wave_of<WAVES>();
   const Row mine = row_of(a, qs, kv, row + 32 * wave + (lane & 31));
-  const bool work = row + 32 * wave < qs.len * a.group;
+  const bool work = WAVES == 1 || row + 32 * wave < qs.len * a.group;
   sk.fetch(k + (int64_t)begin * a.k_row, a.k_row, end - begin, a.head_dim);
   sv.fetch(v + (int64_t)begin * a.v_row, a.v_row, end - begin, a.head_dim);
   Rows<DP> q, dout;
@@ -373,6 +429,27 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cross_bwd_q(Args a) {
   }
   const int64_t at = mine.head * a.q_tokens + mine.token;
   const float lse2 = mine.there ? row_base2(a.lse[at]) : 0.f;
+  // dS of 32 keys from key j on
+  auto weights = [&](char* lds_k, int j) {
+    f32x16 s[2];                                                      // scores, and dP
+    matrix_work(true);
+    products<DP, 2, S::TILE>(s, lds_k, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
+    matrix_work(false);
+    if (WAVES == 1 && hidden(s[0])) without_infinities<DP, 32, 64>(lds_k);       // for dq; nothing else reads them now
+    if (j + 32 > end) {
+      int most = end - 1 - j - 4 * half;
+      asm volatile("" : "+v"(most));
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (walked(r, 0) > most) s[0][r] = -INFINITY;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2));
+    if (ks.len <= 32) delta = own_delta(s[0], s[1]);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[0][r] *= s[1][r] - delta;
+    return rounded(s[0]);
+  };
   f32x16 acc[DP / 32];
 #pragma unroll
   for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
@@ -389,25 +466,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cross_bwd_q(Args a) {
     for (int sub = 0; sub < S::PER; sub += 32) {
       const int j = j0 + sub;
       if (!work || j >= end) break;
-      const char* lds_k = lds + turn + sub * Layout<DP>::PITCH;
-      f32x16 s[2];                                                  // scores, and dP
+      char* const lds_k = lds + turn + sub * Layout<DP>::PITCH;
+      const Weights ds = weights(lds_k, j);
       matrix_work(true);
-      products<DP, 2, S::TILE>(s, lds_k, [&](int n, int i, int) { return n ? dout.f[i] : q.f[i]; });
-      matrix_work(false);
-      if (j + 32 > end) {
-        int most = end - 1 - j - 4 * half;
-        asm volatile("" : "+v"(most));
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (walked(r, 0) > most) s[0][r] = -INFINITY;
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -lse2));
-      if (ks.len <= 32) delta = own_delta(s[0], s[1]);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[0][r] *= s[1][r] - delta;
-      matrix_work(true);
-      accumulate<DP, 1, 0>({&acc}, lds_k, {rounded(s[0])});
+      accumulate<DP, 1, 0>({&acc}, lds_k, {ds});
       matrix_work(false);
     }
     if (more) {
@@ -415,6 +477,27 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cross_bwd_q(Args a) {
       sv.put(lds + (turn ^ 2 * S::TILE) + S::TILE);
     }
     __syncthreads();
+  }
+  if constexpr (WAVES > 1) {
+    __shared__ int32_t said[WAVES];
+    if (any_lane(mine.there && no_number(acc), said)) {
+#pragma unroll
+      for (int m = 0; m < DP / 32; ++m) acc[m] = zeros16();
+      for (int j = begin; j < end; j += 32) {
+        sk.fetch(k + (int64_t)j * a.k_row, a.k_row, end - j, a.head_dim);
+        sv.fetch(v + (int64_t)j * a.v_row, a.v_row, end - j, a.head_dim);
+        sk.put(lds);
+        sv.put(lds + S::TILE);
+        __syncthreads();
+        Weights ds;
+        if (work) ds = weights(lds, j);
+        __syncthreads();
+        without_infinities<DP, 32, S::THREADS>(lds);
+        __syncthreads();
+        if (work) accumulate<DP, 1, 0>({&acc}, lds, {ds});
+        __syncthreads();
+      }
+    }
   }
   if (mine.there && half == 0 && w.share == 0) a.delta[at] = delta;
   if (ks.len > a.share) store_part<DP>(a.parts + (w.part + w.share * a.part_rows + row + 32 * wave + (lane & 31)) * DP, acc, mine.there);
@@ -454,8 +537,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cross_bwd_kv(Args a) {
   float next_lse = 0.f, next_delta = 0.f;
   const bool there = row + 32 * wave + (lane & 31) < ks.len, work = row + 32 * wave < ks.len;
   char* const own = lds + TILE * wave;                               // 32 rows of the wave's, before and after the walk
-  int head = kv * a.group + (all ? first_step / of_head : 0), i = all ? first_step % of_head * STEP : 0, next = i;      // what is fetched next, and the rows under way
-  int at = i;                                                       // what is used now
+  // what is fetched next, the rows under way, what is used now
+  int head, i, next, at;
+  auto start = [&] {
+    head = kv * a.group + first_step / of_head;
+    i = next = at = first_step % of_head * STEP;
+  };
   auto fetch = [&] {
     const int64_t from = (int64_t)qs.first + i;
     sq.fetch(a.q + from * a.q_row + head * a.q_head, a.q_row, qs.len - i, a.head_dim);
@@ -481,6 +568,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cross_bwd_kv(Args a) {
 #pragma unroll
   for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
   if (steps > 0) {
+    start();
     fetch();
     char* const own_v = lds_v + TILE * wave;
     Rows<DP> k, v;
@@ -501,46 +589,76 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cross_bwd_kv(Args a) {
       if (!V_IN_LDS) take_rows<DP>(own, v);
     }
     __syncthreads();
+    // dS and P of the 32 queries at `now`
+    auto weights = [&](char* now, Weights (&w)[2]) {
+      f32x16 s[2];                                                    // scores, and dP
+      matrix_work(true);
+      products<DP, 2, TILE>(s, now, [&](int which, int p, int base) {
+        if (!which) return k.f[p];
+        return V_IN_LDS ? *reinterpret_cast<const bf16x8*>(own_v + (base ^ p << 5)) : v.f[p];
+      });
+      matrix_work(false);
+      if (WAVES == 1 && hidden(s[0])) without_infinities<DP, 32, 64>(now);       // for dk; nothing else reads them now
+      // zeros past the last query times a key that is hidden by minus infinity are no numbers
+      if (at + 32 > qs.len) {
+        int most = qs.len - 1 - at - 4 * half;
+        asm volatile("" : "+v"(most));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (walked(r, 0) > most) s[0][r] = -INFINITY;
+      }
+      const float* scalars = reinterpret_cast<const float*>(now + 2 * TILE) + 4 * half;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 l = *reinterpret_cast<const f32x4*>(scalars + 8 * g), d = *reinterpret_cast<const f32x4*>(scalars + STEP + 8 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * g + e;
+          s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
+          s[1][r] = s[0][r] * (s[1][r] - d[e]);
+        }
+      }
+      w[0] = rounded(s[1]);
+      w[1] = rounded(s[0]);
+    };
     put(lds);
     __syncthreads();
     for (int n = steps, turn = 0; n > 0; --n, turn ^= 1) {
-      const char* const now = lds + turn * BOTH;
+      char* const now = lds + turn * BOTH;
       if (n > 1) fetch();
       if (work) {
-        f32x16 s[2];                                                  // scores, and dP
+        Weights w[2];
+        weights(now, w);
         matrix_work(true);
-        products<DP, 2, TILE>(s, now, [&](int which, int p, int base) {
-          if (!which) return k.f[p];
-          return V_IN_LDS ? *reinterpret_cast<const bf16x8*>(own_v + (base ^ p << 5)) : v.f[p];
-        });
-        matrix_work(false);
-        // zeros past the last query times a key that is hidden by minus infinity are no numbers
-        if (at + 32 > qs.len) {
-          int most = qs.len - 1 - at - 4 * half;
-          asm volatile("" : "+v"(most));
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (walked(r, 0) > most) s[0][r] = -INFINITY;
-        }
-        const float* scalars = reinterpret_cast<const float*>(now + 2 * TILE) + 4 * half;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 l = *reinterpret_cast<const f32x4*>(scalars + 8 * g), d = *reinterpret_cast<const f32x4*>(scalars + STEP + 8 * g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 4 * g + e;
-            s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, -l[e]));
-            s[1][r] = s[0][r] * (s[1][r] - d[e]);
-          }
-        }
-        matrix_work(true);
-        accumulate<DP, 2, TILE>({&dk, &dv}, now, {rounded(s[1]), rounded(s[0])});
+        accumulate<DP, 2, TILE>({&dk, &dv}, now, w);
         matrix_work(false);
       }
       at += STEP;
       if (at >= qs.len) at = 0;
       if (n > 1) put(lds + (turn ^ 1) * BOTH);
       __syncthreads();
+    }
+    if constexpr (WAVES > 1) {
+      __shared__ int32_t said[WAVES];
+      if (any_lane(there && no_number(dk), said)) {
+#pragma unroll
+        for (int m = 0; m < DP / 32; ++m) dk[m] = dv[m] = zeros16();
+        start();
+        for (int n = steps; n > 0; --n) {
+          fetch();
+          put(lds);
+          __syncthreads();
+          Weights w[2];
+          if (work) weights(lds, w);
+          __syncthreads();
+          without_infinities<DP, 32, 64 * WAVES>(lds);
+          __syncthreads();
+          if (work) accumulate<DP, 2, TILE>({&dk, &dv}, lds, w);
+          at += STEP;
+          if (at >= qs.len) at = 0;
+          __syncthreads();
+        }
+      }
     }
   }
   const int64_t first = (int64_t)ks.first + row + 32 * wave;
@@ -594,7 +712,7 @@ __global__ __launch_bounds__(256) void k_cross_join_keys(Args a) {
 // for any rows, and 131 since its rows are stored whole and past the caches.  Two or three tiles of rows need the registers of two waves (256 captions of up to 77: 148 us for 120).
 template <int DP>
 struct Few {
-  static constexpr int WAVES = 4, SUB = 32 * Layout<DP>::PITCH, OWN = 2 * SUB, EACH = 2 * SUB, LDS = OWN + WAVES * EACH;
+  static constexpr int WAVES = 4, SUB = 32 * Layout<DP>::PITCH, OWN = 3 * SUB, EACH = 2 * SUB, LDS = OWN + WAVES * EACH;
   static_assert(32 * Layout<32>::PITCH <= SUB);                      // dS in the place of the values
   static_assert(2 * DP * 128 <= LDS);                                // what join() hands over
 };
@@ -635,7 +753,7 @@ template <int DP>
 __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_cross_bwd_few(Args a) {
   using F = Few<DP>;
   constexpr int SUB = F::SUB, ROUND = 32 * F::WAVES;
-  __shared__ __attribute__((aligned(16))) char lds[F::LDS];           // rows of q, of do; every wave's keys and values, then dS
+  __shared__ __attribute__((aligned(16))) char lds[F::LDS];           // rows of q, of do, of q for dk; every wave's keys and values, then dS
   __shared__ __attribute__((aligned(16))) float row_lse[32], row_delta[32];
   Walk w;
   if (!walk_of<32>(a, w)) return;
@@ -666,10 +784,14 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_cross_bwd_few(Args a) 
 #pragma unroll
       for (int e = 0; e < 8; ++e) delta = fmaf((float)o.f[s][e], (float)dout.f[s][e], delta);
     delta += other_half(delta);
+    const float lse = mine.there ? a.lse[mine.head * a.q_tokens + mine.token] : 0.f;
     put_rows<DP>(lds, q);
     put_rows<DP>(lds + SUB, dout);
+    put_rows<DP>(lds + 2 * SUB, q);
+    // rows that see nothing, maybe for an infinity of their own
+    if (__any(lse == -INFINITY)) without_infinities<DP, 32, 64>(lds + 2 * SUB);
     if (half == 0) {
-      row_lse[lane] = mine.there ? row_base2(a.lse[mine.head * a.q_tokens + mine.token]) : INFINITY;
+      row_lse[lane] = mine.there ? row_base2(lse) : INFINITY;
       row_delta[lane] = delta;
     }
   }
@@ -694,6 +816,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_cross_bwd_few(Args a) 
     if (rows > 0) {
       f32x16 s[2];                                                    // scores, and dP
       products<DP, 2, SUB>(s, lds, [&](int n, int p, int) { return n ? rv.f[p] : rk.f[p]; });
+      if (hidden(s[0])) without_infinities<DP, 32, 64>(own);           // for dq; nothing else reads them now
       // rows past the last are zeros, which times a key that is hidden by minus infinity are no numbers; keys past the last are in no row's softmax
       if (j + 32 > end || rows < 32) {
         int most = key < end ? rows - 1 - 4 * half : -1;
@@ -721,7 +844,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_cross_bwd_few(Args a) 
         for (int e = 0; e < 4; ++e) s[1][4 * g + e] = s[0][4 * g + e] * (s[1][4 * g + e] - d[e]);
       }
       const Weights ds = rounded(s[1]);
-      accumulate<DP, 2, SUB>({&dk, &dv}, lds, {ds, p});
+      accumulate<DP, 2, -SUB>({&dk, &dv}, lds + 2 * SUB, {ds, p});
       accumulate<DP, 1, 0>({&dq}, own, {transposed(weights, ds)});
     }
     store_rows<DP>(own, a.dk + (int64_t)(ks.first + j) * a.k_row + kv * a.k_head, a.k_row, end - j, dk, a.scale, a.head_dim, a.stream);
