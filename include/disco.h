@@ -414,7 +414,7 @@ DISCO_API int disco_embedding_bwd(const disco_embedding_shape* shape, const void
  * as a class token's may be, is not rotated.  Angles are the caller's: of one axis or two, of any base.
  * Element (row, head, channel) of q is at row q_row + head q_head + channel, of qn at qn_row and qn_head; dq lies as q and dqn as qn; k alike.  q, k, dq, dk have
  * x_dtype, qn, kn, dqn, dkn y_dtype; the rest is fp32.
- * head_dim and rotated multiples of 8, head_dim up to 256, strides multiples of 8 up to 2^40, data and rotation 16-byte aligned.  tokens < 2^31.
+ * head_dim and rotated multiples of 8, head_dim up to 256, heads and kv_heads up to 2^16, strides multiples of 8 up to 2^40, data and rotation 16-byte aligned.  tokens < 2^31.
  * Each head's loads come before its stores: an output may be one of its inputs of the same type and strides (qn = q, dq = dqn, dq = q).
  *
  * disco_head_norm_bwd: q and k of the forward call (not read, and may be NULL, without a norm), dqn and dkn.  Writes dq and dk, and where not NULL dw_q, db_q, dw_k and

@@ -352,13 +352,5 @@ __device__ __forceinline__ void take_rows(const char* lds, Rows<DP>& r) {
   for (int s = 0; s < DP / 16; ++s) r.f[s] = *reinterpret_cast<const bf16x8*>(lds + (base ^ s << 5));
 }
 
-// Between lanes of a wave that write rows into the LDS and lanes that read them there, either way round: what was issued before this is done before what
-// comes after it.  One wave's LDS instructions keep their order by themselves, so this is no instruction; it is what keeps the compiler to it.
-__device__ __forceinline__ void wave_exchange() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-}
-
 }  // namespace
 }  // namespace disco

@@ -66,6 +66,14 @@ __device__ __forceinline__ V wave_reduce(V v, F f) {
   return f(__builtin_bit_cast(V, q0), __builtin_bit_cast(V, q1));
 }
 
+// Between lanes of a wave that write rows into the LDS and lanes that read them there, either way round: what was issued before this is done before what
+// comes after it.  One wave's LDS instructions keep their order by themselves, so this is no instruction; it is what keeps the compiler to it.
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Stores a result; `stream`: past the caches, for results so large that nothing would be found there.  (The empty asm keeps the compiler from making one
 // store of the two, which is then no streaming one.)
 template <class T, class V>

@@ -52,9 +52,9 @@ struct Args {
 };
 
 struct Range { int first, len; };
+__device__ __forceinline__ int bounded(int start, int64_t tokens) { return start < 0 ? 0 : start > (int)tokens ? (int)tokens : start; }
 __device__ __forceinline__ Range range_of(const int32_t* starts, int64_t tokens, int longest, int s) {
-  const int most = (int)tokens, x = starts[s], y = starts[s + 1];
-  const int from = x < 0 ? 0 : x > most ? most : x, to = y < 0 ? 0 : y > most ? most : y, len = to - from;
+  const int from = bounded(starts[s], tokens), len = bounded(starts[s + 1], tokens) - from;
   Range r;
   r.first = __builtin_amdgcn_readfirstlane(from);
   r.len = __builtin_amdgcn_readfirstlane(len < 0 ? 0 : len < longest ? len : longest);
@@ -64,8 +64,8 @@ __device__ __forceinline__ Range range_of(const int32_t* starts, int64_t tokens,
 // Sequences own slots, sequence s those from starts[s] each / T + s on: at least as many as it has tiles of T rows, `each` of them to a token, whatever its start,
 // so that they are found with no table.  The sequence that owns one, searched for 64 ways at once, and which of its slots it is; false: no sequence.
 __device__ __forceinline__ bool find_slot(const int32_t* starts, int64_t tokens, int sequences, int each, int T, int slot, int& s, int& index) {
-  const int lane = threadIdx.x & 63, most = (int)tokens;
-  auto first = [&](int i) { const int v = starts[i]; return (v < 0 ? 0 : v > most ? most : v) * each / T + i; };
+  const int lane = threadIdx.x & 63;
+  auto first = [&](int i) { return bounded(starts[i], tokens) * each / T + i; };
   int lo = 0, n = sequences;
   for (;;) {
     const int step = (n + 63) / 64, i = lo + lane * step;
@@ -327,7 +327,6 @@ __global__ __launch_bounds__(256) void k_cross_join_rows(Args a) {
     token = (int)(in / a.group);
     head = kv * a.group + (int)(in % a.group);
     const int s = sequence_of(a.q_starts, a.sequences, token);
-    auto bounded = [](int v, int64_t most) { return v < 0 ? 0 : v > (int)most ? (int)most : v; };
     const int q0 = bounded(a.q_starts[s], a.q_tokens), q1 = bounded(a.q_starts[s + 1], a.q_tokens);
     const int k0 = bounded(a.k_starts[s], a.k_tokens), k1 = bounded(a.k_starts[s + 1], a.k_tokens);
     const int len = k1 - k0 < a.k_longest ? k1 - k0 : a.k_longest;
@@ -680,7 +679,6 @@ __global__ __launch_bounds__(256) void k_cross_join_keys(Args a) {
   const bool values = piece * 8 >= DP;
   if (at >= rows) return;
   const int kv = (int)(at / a.k_tokens), token = (int)(at % a.k_tokens), s = sequence_of(a.k_starts, a.sequences, token);
-  auto bounded = [](int v, int64_t most) { return v < 0 ? 0 : v > (int)most ? (int)most : v; };
   const int q0 = bounded(a.q_starts[s], a.q_tokens), q1 = bounded(a.q_starts[s + 1], a.q_tokens);
   const int k0 = bounded(a.k_starts[s], a.k_tokens), k1 = bounded(a.k_starts[s + 1], a.k_tokens);
   const int len = q1 - q0 < 0 ? 0 : q1 - q0 < a.q_longest ? q1 - q0 : a.q_longest, all = (len + STEP - 1) / STEP * a.group;

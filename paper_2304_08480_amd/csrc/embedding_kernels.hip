@@ -103,12 +103,6 @@ __device__ __forceinline__ uint64_t lanes_like(int v, int bits) {
   return same;
 }
 __device__ __forceinline__ int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
-// Between lanes of a wave that write the LDS and lanes that read it.
-__device__ __forceinline__ void wave_exchange() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-}
 
 // Gradients of ids that do not occur are zeros: workgroups beside those that sort, which wait for the LDS and leave the memory idle, clear everything (101 MB of
 // gradients, 26 thousand rows of 512, forward and backward: 80 us for 87 with the rows that do not occur cleared by those that sort).  Each launch has a share,
@@ -299,7 +293,7 @@ template <int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_embedding_order(Gradients a, int slices) {
   constexpr int N = 64 * WAVES;
   extern __shared__ int32_t counts[];                                // wave, local id: rows, then the next one's place in the list
-  __shared__ int32_t totals[MOST_LOCAL], sums[WAVES], ends[WAVES][64];
+  __shared__ int32_t sums[WAVES], ends[WAVES][64];
   if ((int)blockIdx.x >= slices) {
     clear_share(a, a.cleared, a.to_clear, blockIdx.x - slices, gridDim.x - slices);
     return;
@@ -336,10 +330,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_embedding_order(Gradients a, int
   for (int from = 0; from < local; from += N) {
     const int l = from + threadIdx.x;
     int total = 0;
-    if (l < local) {
+    if (l < local)
       for (int w = 0; w < WAVES; ++w) total += counts[w * local + l];
-      totals[l] = total;
-    }
     int upto = total;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
