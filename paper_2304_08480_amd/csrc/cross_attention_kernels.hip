@@ -14,14 +14,17 @@
 //
 // Bound by memory: the matrix instructions have a tenth of the time and vector instructions a quarter.  Heads are pieces of 128 or 256 bytes of a row; a plain
 // reader of such pieces reaches 5.5 to 5.7 TB/s.  Here a workgroup waits for its starts, its rows, its first tiles, one after the other.  In microseconds:
-//   512 images, one query each over 197 rows, 12 heads of 64: forward 59 (5.3 TB/s), backward 131 (4.8; keys and values read once, their gradients written);
-//   256 captions of 4 to 77 over 197 rows, 12 heads of 64: forward 39, dq 41, dk and dv 69;
-//   16 x 64 latents over 1 to 8192 rows, 16 heads of 128 on 8: forward 31 to 40 and 12 for the joint, dq 37 and 10, dk and dv 55;
-//   one query of 4 sequences of up to 16384, 16 heads of 128 on 2, forward: 13 and 7.
+//   512 images, one query each over 197 rows, 12 heads of 64: forward 58 (5.3 TB/s), backward 130 (4.8; keys and values read once, their gradients written);
+//   256 captions of 4 to 77 over 197 rows, 12 heads of 64: forward 39, dq 43, dk and dv 60;
+//   16 x 64 latents over 1 to 8192 rows, 16 heads of 128 on 8: forward 33 to 40 and 12 for the joint, dq 38 and 10, dk and dv 58;
+//   one query of 4 sequences of up to 16384, 16 heads of 128 on 2, forward: 13 to 14 and 7 to 8.
+// Many queries on many keys are bound by the products and what stands between them: 2 x 3000 on 3000, 8 heads of 64, forward and backward 241 to 253 (510 to 535 TFLOP/s), 4 x 2048
+// on 4096, 16 heads of 128, 1160 (830).
 // Keys and values are read for the last time by the kernels that write their gradients, which do not keep them in the caches; nor do they keep
-// large dk and dv there (STREAM).  The images, forward and backward, take 182 us so, 199 if keys and values are kept, 220 if the gradients are too: the next forward pass
+// large dk and dv there (STREAM).  The images, forward and backward, took 182 us so, 199 if keys and values are kept, 220 if the gradients are too: the next forward pass
 // waits for what was left in the caches to be written.
-// The second reading, for dk and dv, is from the last-level cache: both sides in one launch, one behind the other, took 123 for the captions' 120.
+// The second reading, for dk and dv, is from the last-level cache: both sides in one launch, one behind the other, took 123 where the captions' two launches took 120 (before rows were
+// staged and stored whole).
 //
 // Scores, softmax and sums are fp32, P and dS are rounded to bf16 for the matrix instruction, as in attention_kernels.hip: against 64 bits o and the gradients
 // are off by 0.0023 to 0.0024 of their norm (in fp32 throughout by 0.0017, their own rounding to bf16).
@@ -706,8 +709,9 @@ __global__ __launch_bounds__(256) void k_cross_join_keys(Args a) {
 
 // ---- backward with few rows: all rows of a sequence and key head, up to 32, stand in the LDS of one workgroup, whose waves walk the keys, 32 at a time.
 // A key's dk and dv are then whole at once, every key and value is read one time, and S and dP are taken one time for all three gradients: dS goes through the
-// LDS to be the other operand of dq's product (5 products for 7).  One query over 197 rows, 512 times, 12 heads of 64: 155 us for the 59 and 171 of the two kernels
-// for any rows, and 131 since its rows are stored whole and past the caches.  Two or three tiles of rows need the registers of two waves (256 captions of up to 77: 148 us for 120).
+// LDS to be the other operand of dq's product (5 products for 7).  One query over 197 rows, 512 times, 12 heads of 64, forward and backward: 180 us, 218 with
+// the two kernels for any rows.  Two or three tiles of rows need the registers of two waves (256 captions of up to 77, tried before rows were stored whole: 148 us where the two
+// kernels took 120).
 template <int DP>
 struct Few {
   static constexpr int WAVES = 4, SUB = 32 * Layout<DP>::PITCH, OWN = 3 * SUB, EACH = 2 * SUB, LDS = OWN + WAVES * EACH;
@@ -908,8 +912,8 @@ void cut_rows(int64_t rows, int64_t longest, int64_t sequences, int T, Plan& p) 
   p.slots = p.tiles ? each * sequences : found;
 }
 
-// Half of what the chip has room for: cut in two they would take as long again.  (2 x 3000 queries on 3000 keys, 8 heads of 64, 384 workgroups for dk and dv: 260 us
-// forward and backward, 282 if they are cut.)
+// Half of what the chip has room for: cut in two they would take as long again.  (2 x 3000 queries on 3000 keys, 8 heads of 64, 384 workgroups for dk and dv: 253 us
+// forward and backward, 275 if they are cut.)
 bool enough(int64_t workgroups, int64_t room) { return 2 * workgroups > room; }
 // The share of a walk in units (keys, or steps of queries), `longest` and on average `mean` of them: as many workgroups as the chip has room for, `least`
 // units to a share, which is a whole number of steps, and no more shares than `most`, nor, as every sequence has as many, than four times that room.
@@ -960,11 +964,11 @@ Plan plan_rows(const Args& a) {
   Plan p = {};
   const int64_t rows = a.q_tokens * a.group, longest = (int64_t)a.q_longest * a.group, mean = rows / a.sequences;
   // Tiles of 128 rows read the keys once for four of 32; where most rows are fewer than that, a wave alone.  200 captions of 1 to 60, 22 on average, over 197 rows, 8
-  // heads of 64, forward and backward: 82 us, with four waves 87; 100 of 40, heads of 128: 105, with one 114.
+  // heads of 64, forward and backward: 75 us, with four waves 79; 100 of 40, heads of 128: 96, with one 104.
   p.waves = longest <= 32 || mean <= 24 ? 1 : 4;
   cut_rows(rows, longest, a.sequences, 32 * p.waves, p);
-  // Shares of 256 keys for one wave and 512 for four, which leave 4 times as many rows of parts each: 64 latents over up to 8192, forward and backward, 161 us; of
-  // 256 185, 320 168.  One token's, 256 20 us, 128 21, 64 23.
+  // Shares of 256 keys for one wave and 512 for four, which leave 4 times as many rows of parts each: 64 latents over up to 8192, forward and backward, 149 us; of
+  // 256 159, of 1024 160.  One token's, 256 20 us, 128 21, 64 23.
   const int step = p.waves == 1 ? 32 : 64, least = p.waves == 1 ? 256 : 512, room = p.waves == 1 ? 4 * COMPUTE_UNITS : 2 * COMPUTE_UNITS;
   cut_keys(a, p.slots * a.kv_heads, room, least, step, padded(a) * sizeof(float) + sizeof(f32x2), p);
   return p;
@@ -977,7 +981,7 @@ Plan plan_keys(const Args& a) {
   const int64_t workgroups = p.slots * a.kv_heads;
   const int64_t longest = (a.q_longest + STEP - 1) / STEP * (int64_t)a.group, middle = (a.q_tokens / a.sequences + STEP - 1) / STEP * a.group;
   const size_t bytes = (size_t)a.k_tokens * a.kv_heads * 2 * padded(a) * sizeof(float);
-  // 8 steps at least: 5000 queries on 20 keys, 8 heads of 64, forward and backward 29 us, with 4 26, 16 37, all in one 59; 9000 on 77, 45, 52, 49 and 307
+  // 8 steps at least: 5000 queries on 20 keys, 8 heads of 64, forward and backward 31 us, with 4 30, 16 38, all in one 178; 9000 on 77, 46, 47, 50 and 313
   p.share = share_of(workgroups, 2 * COMPUTE_UNITS, middle, longest, 8, 1, (int64_t)(MOST_PARTS / bytes));
   p.shares = (int)((longest + p.share - 1) / p.share);
   p.bytes = p.shares > 1 ? p.shares * bytes : 0;

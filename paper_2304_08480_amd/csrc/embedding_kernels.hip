@@ -3,7 +3,7 @@
 //   y_i = scale E[id_i] + P[place_i],   dE[v] = scale sum of dy_i over id_i = v,   dP[p] = sum of dy_i over place_i = p
 //
 // Forward: a gather, bound by the rows written and by what the pass before has left of the table in the caches (26533 rows of 512 bf16 from fp32 tables: 12 us one
-// call behind the other, 14 after a backward pass, which writes 100 MB; 78848 rows of 768: 53 after one).
+// call behind the other, 14 to 16 after a backward pass, which writes 100 MB; 78848 rows of 768: 52 after one).
 //
 // Backward, both tables in the same launches (microseconds for those two batches, vocabulary 49408, gradients fp32):
 //   deal   blocks of 2048 rows, sorted in the LDS by their ids' low bits into `slices`, rows rising inside each.  Low bits, because the frequent ids, which
@@ -39,7 +39,7 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int64_t i, int wide) {
 
 constexpr int THREADS = 256;
 // A row's lanes, LANES of 8 columns each.  One row at a time for a group of lanes: waves enough are on the chip to keep the memory busy with one each (26 thousand rows
-// of 512 forward and backward 72.5 us, with two rows asked for at once 72.7, with four 74.0, with eight 78).
+// of 512, when forward and backward took 72.5 us: with two rows asked for at once 72.7, with four 74.0, with eight 78).
 template <bool TABLE_BF16, bool Y_BF16, int LANES, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void k_embedding(Lookup a) {
   constexpr int GROUPS = THREADS / LANES;
@@ -105,7 +105,7 @@ __device__ __forceinline__ uint64_t lanes_like(int v, int bits) {
 __device__ __forceinline__ int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
 
 // Gradients of ids that do not occur are zeros: workgroups beside those that sort, which wait for the LDS and leave the memory idle, clear everything (101 MB of
-// gradients, 26 thousand rows of 512, forward and backward: 80 us for 87 with the rows that do not occur cleared by those that sort).  Each launch has a share,
+// gradients, 26 thousand rows of 512, when this was tried: forward and backward 80 us for 87 with the rows that do not occur cleared by those that sort).  Each launch has a share,
 // counted in pieces of 16 KiB.
 constexpr int CLEAR = 16384;
 __device__ __forceinline__ void clear_pieces(const Gradients& a, int64_t from, int64_t to) {

@@ -3,8 +3,8 @@
 //   n = N(x) over a head's channels,  y = R n:  a' = a cos - b sin,  b' = a sin + b cos for every pair (a, b) of rotated channels
 //   g = R^T dy,  dx = rstd (p - [mean p] - xhat mean(p xhat)),  p = g w,  xhat = (x - mean) rstd;  dw = sum g xhat,  db = sum g
 //
-// Bound by memory, at the rate of a copy (128 x 197 rows, 12 and 12 heads of 64, layer norms, bf16: forward 35 us, 4.5 TB/s, backward 46, 5.1, and 5 for the sums; 4 x 8192
-// rows, 16 and 8 heads of 128, RMS: 84 and 104 us, 4.8 and 5.8, and 6; 13 x 769 rows, 5 heads and 1 of 80, fp32 to bf16: 12 us, 2.4, where 6 of 16 lanes have no
+// Bound by memory, at the rate of a copy (128 x 197 rows, 12 and 12 heads of 64, layer norms, bf16: forward 35 to 37 us, 4.2 to 4.5 TB/s, backward 46, 5.1, and 5 for the sums; 4 x 8192
+// rows, 16 and 8 heads of 128, RMS: 82 and 102 us, 4.9 and 5.9, and 6; 13 x 769 rows, 5 heads and 1 of 80, fp32 to bf16: 12 us, 2.4, where 6 of 16 lanes have no
 // channels and no two heads of a unit need be of one row).  A head is read once, kept by LANES lanes, 8 channels each, and written once.  A lane has both channels of its pairs, whichever way they
 // are paired: pairs of halves are two loads of four channels, half the rotated width apart.  The norm is two exchanges between those lanes.
 // A group of lanes takes HEADS heads at once, so that its loads are under way together; those of one row share cosines and sines.  The
